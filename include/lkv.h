@@ -8,7 +8,8 @@
  * the uncompacted cache, the training-time attention kernel with that mask
  * (forward and backward), the LKV-H budget allocation with the forward
  * Soft-TopK operator and its backward pass, and the observation-window scorer that the paper's
- * ablation runs under the same budgets (lkv_score_window).
+ * ablation runs under the same budgets (lkv_score_window); and the packed cache in 8 bits
+ * (lkv_compact_quant, lkv_append_quant, lkv_decode_attn_quant, lkv_reevict_quant) and rotary positions (lkv_rope).
  *
  * General conventions
  * -------------------
@@ -369,6 +370,126 @@ lkv_status lkv_reevict(lkv_ctx *ctx, int64_t n_segments, int32_t head_dim, const
                        const int32_t *lengths_host, const int32_t *new_budgets, int32_t slack,
                        int32_t *idx, int32_t *offsets, void *kp_new, void *vp_new, float *up_new,
                        int32_t *cap_offsets_new, int32_t *lengths_new, int64_t *total_kept, void *stream);
+
+/* ---- The packed cache in 8 bits -------------------------------------------------------------
+ * The same ragged cache with one byte per value: half the memory, and half the bytes that a decode step reads.  Segments,
+ * offsets, slack and growth are those of the bf16 cache above.  Every LKV_QUANT_BLOCK = 32 rows of a segment, counted from its
+ * first row, are a block with one fp32 scale for their keys and one for their values: value = code * scale.
+ *   LKV_QUANT_E4M3 : codes are 8-bit floating-point numbers (4 exponent and 3 mantissa bits, no infinities, largest 448):
+ *                    relative error up to 2^-4, whatever else is in the block; the choice for keys with outlier channels
+ *   LKV_QUANT_INT8 : codes are whole numbers in [-127, 127]: error up to half a scale, i.e. up to 1/127 of the block's
+ *                    largest magnitude; two to three times as exact as e4m3 for values of one size
+ * A scale is the smallest power of two s with max |value| <= 448 s (127 s), at least 2^-126, and 0 for a block of zeros; a code
+ * is value / s rounded to nearest even.  So codes and scales are unique, and reproducible bit for bit.  A NaN is stored as 0
+ * and an infinity as the largest code, and neither counts for the scale.
+ * Scale of block b of segment s: number cap_offsets[s] / 32 + s + b of k_scale and v_scale, which hold
+ * lkv_quant_scales(n_segments, total_rows) = total_rows / 32 + n_segments numbers (total_rows: all rows, spare ones too);
+ * some numbers belong to no block and are left as they were, and so are spare rows. */
+#define LKV_QUANT_BLOCK 32
+typedef enum { LKV_QUANT_E4M3 = 0, LKV_QUANT_INT8 = 1 } lkv_quant_format;
+typedef struct {      /* HOST struct of DEVICE pointers, 16-byte aligned */
+  int32_t format;     /* lkv_quant_format */
+  void *k, *v;        /* DEVICE, one byte per value [total_rows, 128] */
+  float *k_scale;     /* DEVICE fp32 [lkv_quant_scales(n_segments, total_rows)] */
+  float *v_scale;     /* DEVICE fp32, as many */
+} lkv_quant_rows;
+int64_t lkv_quant_scales(int64_t n_segments, int64_t total_rows);
+
+/* lkv_compact (slack = 0) or lkv_compact_grow into a packed 8-bit cache: row j of segment s goes to row
+ * offsets[s] + slack * s + j.
+ * idx, offsets : DEVICE, as written by lkv_select
+ * packed       : of total_kept + n_segments * slack rows
+ * up           : NULL, or DEVICE fp32 of as many rows: receives the kept rows' scores, as lkv_reevict_quant needs them
+ * scores       : HOST [n_seq] of DEVICE fp32 [L, H, T_s], the scores the selection used; read if up is given, else may be NULL
+ * cap_offsets, lengths : DEVICE int32 [n_segments + 1] and [n_segments], written as by lkv_compact_grow; both may be NULL
+ *                without slack (offsets then is the table that lkv_decode_attn_quant takes) */
+lkv_status lkv_compact_quant(lkv_ctx *ctx, const lkv_cache *cache, const float *const *scores, const int32_t *idx,
+                             const int32_t *offsets, int64_t total_kept, int32_t slack, const lkv_quant_rows *packed,
+                             float *up, int32_t *cap_offsets, int32_t *lengths, void *stream);
+
+/* lkv_decode_attn (lengths = NULL: segment s is rows cap_offsets[s] .. cap_offsets[s+1]) or lkv_decode_attn_grown over a
+ * packed 8-bit cache.  bf16 queries; the products, softmax and sums are those of fp32 on the exact values code * scale, to
+ * about 1e-5 (probabilities are multiplied in two bf16 parts).  Any finite scales >= 0 are taken here.  scale: finite.
+ * total_rows : cap_offsets[n_segments]
+ * workspace  : DEVICE, at least lkv_decode_quant_workspace_bytes(...) bytes, 256-byte aligned; need not be initialised */
+size_t lkv_decode_quant_workspace_bytes(int32_t n_segments, int64_t total_rows, int32_t n_q_heads, int32_t n_kv_heads);
+lkv_status lkv_decode_attn_quant(lkv_ctx *ctx, int32_t n_seq, int32_t n_layers, int32_t n_kv_heads, int32_t n_q_heads,
+                                 int32_t head_dim, const void *q, const lkv_quant_rows *packed, const int32_t *cap_offsets,
+                                 const int32_t *lengths, int64_t total_rows, float scale, float *out, float *lse,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* lkv_reevict of a packed 8-bit cache: the same rows are kept, in the same order.  The kept rows' values are quantised in
+ * their new blocks, with the scales that the new blocks' values need: a row whose scale does not grow keeps its values.
+ * packed, packed_new : of the same format; must not overlap.  The scales of `packed` are powers of two or 0, as the calls here
+ *                      write them.  Everything else as for lkv_reevict */
+lkv_status lkv_reevict_quant(lkv_ctx *ctx, int64_t n_segments, int32_t head_dim, const lkv_quant_rows *packed,
+                             const float *up, const int32_t *cap_offsets, const int32_t *lengths,
+                             const int32_t *lengths_host, const int32_t *new_budgets, int32_t slack, int32_t *idx,
+                             int32_t *offsets, const lkv_quant_rows *packed_new, float *up_new,
+                             int32_t *cap_offsets_new, int32_t *lengths_new, int64_t *total_kept, void *stream);
+
+/* ---- Rotary positions ---------------------------------------------------------------------
+ * Channels a and b of pair i, at position p: with angle = p * inv_freq[i] (fp64) and c, s = factor * cos, sin of it,
+ *   y_a = c x_a - s x_b,  y_b = s x_a + c x_b;  the channels from rotary_dim on are copied, bit for bit.
+ * The cached keys of every call above are keys after this; generated tokens' queries and keys go through it as well. */
+typedef enum { LKV_ROTARY_HALVES = 0,   /* pair i: channels i and i + rotary_dim / 2 */
+               LKV_ROTARY_PAIRS = 1     /* pair i: channels 2 i and 2 i + 1 */
+} lkv_rotary_layout;
+typedef struct {           /* HOST struct */
+  int32_t layout;          /* lkv_rotary_layout */
+  int32_t rotary_dim;      /* even, 2 .. 128 */
+  const double *inv_freq;  /* DEVICE fp64 [rotary_dim / 2], radians per position, 16-byte aligned */
+  double factor;           /* 1, or the attention factor of a context extension */
+} lkv_rotary;
+
+/* Frequencies and factor of the usual context extensions, from their published formulas; HOST in, HOST out, no context.
+ * With w_i = base^(-2 i / rotary_dim):
+ *   LKV_ROPE_PLAIN       : w_i
+ *   LKV_ROPE_LINEAR      : w_i / stretch (position interpolation)
+ *   LKV_ROPE_BASE        : base * stretch^(r / (r - 2)) in base's place (NTK-aware; rotary_dim >= 4)
+ *   LKV_ROPE_PARTS       : w_i from pair `first` on, w_i / stretch past pair `last`, a ramp between, where first and last are the
+ *                          pairs (rounded down and up) that make `high` and `low` turns over trained_len (YaRN, usually 32
+ *                          and 1); factor 0.1 ln stretch + 1
+ *   LKV_ROPE_WAVELENGTHS : w_i for pairs of at least `high` turns over trained_len, w_i / stretch for those of at most `low`,
+ *                          and in between by the turns' share of the way (usually 4 and 1)
+ * inv_freq : HOST fp64 [rotary_dim / 2];  factor : HOST, 1 but for LKV_ROPE_PARTS
+ * LKV_ERR_INVALID_ARG for an unknown kind, rotary_dim not even in [2, 128], base <= 1, stretch < 1, trained_len <= 0 or not
+ * 0 < low < high (each only where the kind uses it). */
+typedef enum { LKV_ROPE_PLAIN = 0, LKV_ROPE_LINEAR = 1, LKV_ROPE_BASE = 2, LKV_ROPE_PARTS = 3, LKV_ROPE_WAVELENGTHS = 4 } lkv_rope_kind;
+typedef struct {
+  int32_t kind;         /* lkv_rope_kind */
+  int32_t rotary_dim;
+  double base, stretch, trained_len, low, high;
+} lkv_rope_scaling;
+lkv_status lkv_rope_frequencies(const lkv_rope_scaling *scaling, double *inv_freq, double *factor);
+
+/* Rotates [n_batch, n_heads, n_tokens, 128] of any strides with the channels contiguous.
+ * dtype      : of x and y: LKV_BF16 (q, k) or LKV_FP32 (their gradients as lkv_masked_attn_backward writes them); the
+ *              rotation is fp32 with cosine and sine good to fp32 at any position
+ * x, y       : DEVICE; y may be x (then with the same strides), and must not overlap it otherwise
+ * x_strides, y_strides : HOST int64 [3], elements between batches, heads and tokens; multiples of 16 bytes
+ * positions  : DEVICE int32, position of token t of batch b at [b * positions_stride + t] (stride 0: one row for all);
+ *              or NULL: first_position + t
+ * backward   : 0, or 1: the transposed map, which takes the gradient of y to that of x */
+typedef enum { LKV_BF16 = 0, LKV_FP32 = 1 } lkv_dtype;
+lkv_status lkv_rope(lkv_ctx *ctx, const lkv_rotary *rotary, int32_t dtype, int32_t n_batch, int32_t n_heads,
+                    int32_t n_tokens, int32_t head_dim, const void *x, const int64_t *x_strides, void *y,
+                    const int64_t *y_strides, const int32_t *positions, int64_t positions_stride,
+                    int32_t first_position, int32_t backward, void *stream);
+
+/* lkv_append to a packed 8-bit cache, the key rotated on the way.
+ * rotary, positions : NULL both, or the rotation of k_new and DEVICE int32 [n_seq], the new token's position in each sequence
+ *                     (its place in the whole sequence, not its row).  The rotated key is rounded to bf16, as lkv_rope leaves it,
+ *                     and that is what is scored and stored.
+ * scorer, up        : NULL both (no scores: the cache cannot be re-evicted), or as for lkv_append
+ * The row's block keeps its scales where they hold the new row; where one has to grow, the block's rows are rounded again to
+ * the new scale (they end less than one step of the last scale off).  A block's first row sets its scales.
+ * packed            : scales are powers of two or 0, as the calls here write them
+ * Everything else as for lkv_append (lengths grow by one; a full segment is left untouched and *overflow set). */
+lkv_status lkv_append_quant(lkv_ctx *ctx, int32_t n_seq, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                            const lkv_scorer *scorer, const lkv_rotary *rotary, const int32_t *positions,
+                            const void *k_new, const void *v_new, const lkv_quant_rows *packed, float *up,
+                            const int32_t *cap_offsets, int32_t *lengths, int32_t *overflow, void *stream);
 
 /* ---- Attention with a multiplicative retention mask over the UNCOMPACTED cache (App. B.2) ----
  * For one query per head: p_i = e^{s_i} m_i / sum_j e^{s_j} m_j, s_i = scale * q . K[l, h, i, :],

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblkv.so")
 SOURCES = ["lkv_api.hip", "score_linear.hip", "score_mlp.hip", "score_window.hip", "select.hip", "counts.hip", "compact.hip", "decode.hip", "lkv_h.hip", "append.hip",
-           "masked_attn.hip", "masked_attn_bwd.hip"]
+           "masked_attn.hip", "masked_attn_bwd.hip", "quant_compact.hip", "quant_append.hip", "quant_decode.hip", "rope.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -134,6 +134,43 @@ lkv_status check_attention_geometry(lkv_ctx* ctx, int32_t n_q_heads, int32_t n_k
   return LKV_OK;
 }
 
+// The tensors of a packed 8-bit cache of `rows` rows.
+lkv_status check_quant_rows(lkv_ctx* ctx, const lkv_quant_rows* x, int64_t rows, const char* what) {
+  if (x == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "%s is NULL", what);
+  if (x->format != LKV_QUANT_E4M3 && x->format != LKV_QUANT_INT8)
+    return fail(ctx, LKV_ERR_INVALID_ARG, "%s: unknown format %d", what, x->format);
+  if (rows > 0 && (x->k == nullptr || x->v == nullptr || x->k_scale == nullptr || x->v_scale == nullptr))
+    return fail(ctx, LKV_ERR_INVALID_ARG, "%s: k, v, k_scale or v_scale is NULL", what);
+  if (!aligned16(x->k) || !aligned16(x->v) || !aligned16(x->k_scale) || !aligned16(x->v_scale))
+    return fail(ctx, LKV_ERR_INVALID_ARG, "%s: k, v, k_scale or v_scale is not 16-byte aligned", what);
+  return LKV_OK;
+}
+
+lkv::QuantRows as_quant_rows(const lkv_quant_rows* x) {
+  return {static_cast<uint8_t*>(x->k), static_cast<uint8_t*>(x->v), x->k_scale, x->v_scale};
+}
+
+lkv_status check_quant_total(lkv_ctx* ctx, int64_t rows) {
+  if (rows < 0 || rows >= (int64_t)1 << 31) return fail(ctx, LKV_ERR_INVALID_ARG, "%lld rows are outside [0, 2^31)", (long long)rows);
+  return LKV_OK;
+}
+
+lkv_status check_rotary(lkv_ctx* ctx, const lkv_rotary* r) {
+  if (r == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "rotary is NULL");
+  if (r->layout != LKV_ROTARY_HALVES && r->layout != LKV_ROTARY_PAIRS)
+    return fail(ctx, LKV_ERR_INVALID_ARG, "unknown rotary layout %d", r->layout);
+  if (r->rotary_dim < 2 || r->rotary_dim > lkv::kHeadDim || r->rotary_dim % 2 != 0)
+    return fail(ctx, LKV_ERR_INVALID_ARG, "rotary_dim = %d must be even and lie in [2, 128]", r->rotary_dim);
+  if (r->inv_freq == nullptr || !aligned16(r->inv_freq))
+    return fail(ctx, LKV_ERR_INVALID_ARG, "inv_freq is NULL or not 16-byte aligned");
+  if (!std::isfinite(r->factor)) return fail(ctx, LKV_ERR_INVALID_ARG, "factor must be finite");
+  return LKV_OK;
+}
+
+lkv::RotaryArgs as_rotary(const lkv_rotary* r) {
+  return {r->inv_freq, r->factor, r->rotary_dim, r->layout == LKV_ROTARY_PAIRS ? 1 : 0};
+}
+
 hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
 // lkv_score, optionally counting the first-level top-k digits of every segment on the way (counts zero on entry).
@@ -561,6 +598,54 @@ lkv_status lkv_decode_attn_static(lkv_ctx* ctx, int32_t n_seq, int32_t n_layers,
   return LKV_OK;
 }
 
+}  // extern "C"
+
+namespace {
+
+// Host tables of a re-eviction: the new cache's rows and the longest segment held.
+lkv_status check_reeviction(lkv_ctx* ctx, int64_t n_segments, int32_t head_dim, const int32_t* lengths_host, const int32_t* new_budgets,
+                            int32_t slack, int64_t* total_out, int* max_len_out) {
+  if (head_dim != lkv::kHeadDim) return fail(ctx, LKV_ERR_UNSUPPORTED, "head_dim must be 128, got %d", head_dim);
+  if (n_segments < 1) return fail(ctx, LKV_ERR_INVALID_ARG, "n_segments = %lld must be >= 1", (long long)n_segments);
+  if (n_segments > kMaxSegments) return fail(ctx, LKV_ERR_UNSUPPORTED, "too many segments");
+  if (lengths_host == nullptr || new_budgets == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "lengths_host or new_budgets is NULL");
+  if (slack < 0) return fail(ctx, LKV_ERR_INVALID_ARG, "slack = %d must be >= 0", slack);
+  int64_t total = 0;
+  int max_len = 1;
+  for (int64_t i = 0; i < n_segments; ++i) {
+    if (lengths_host[i] < 0) return fail(ctx, LKV_ERR_INVALID_ARG, "length %d of segment %lld is negative", lengths_host[i], (long long)i);
+    if (new_budgets[i] < 0 || new_budgets[i] > lengths_host[i])
+      return fail(ctx, LKV_ERR_INVALID_ARG, "new budget %d of segment %lld is outside [0, %d]", new_budgets[i],
+                  (long long)i, lengths_host[i]);
+    total += new_budgets[i];
+    if (lengths_host[i] > max_len) max_len = lengths_host[i];
+  }
+  if (total + n_segments * slack >= (int64_t)1 << 31)
+    return fail(ctx, LKV_ERR_UNSUPPORTED, "new cache of %lld rows >= 2^31", (long long)(total + n_segments * slack));
+  *total_out = total;
+  *max_len_out = max_len;
+  return LKV_OK;
+}
+
+// Row numbers that a re-eviction keeps of every segment, and the tight offsets of the new budgets that they are written at.
+lkv_status reevict_select(lkv_ctx* ctx, int64_t n_segments, const int32_t* new_budgets, int max_len, const float* up,
+                          const int32_t* cap_offsets, const int32_t* lengths, int32_t* idx, int32_t* offsets, void* stream) {
+  if (lkv_status st = lkv_plan_offsets(ctx, n_segments, new_budgets, offsets, nullptr, stream)) return st;
+  lkv::SeqTable tab;
+  memset(&tab, 0, sizeof(tab));
+  tab.T[0] = max_len;          // upper bound of every segment's length: sizes the LDS region
+  tab.first[0] = 0;
+  tab.first[1] = (int32_t)n_segments;
+  tab.n = 1;
+  lkv::launch_select(tab, nullptr, (int)n_segments, offsets, idx, 0, 0, as_stream(stream), up, cap_offsets, lengths);
+  if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "re-eviction select launch");
+  return LKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
 lkv_status lkv_plan_offsets(lkv_ctx* ctx, int64_t n_segments, const int32_t* budgets, int32_t* offsets,
                             int64_t* total_kept, void* stream) {
   if (ctx == nullptr) return LKV_ERR_INVALID_ARG;
@@ -794,47 +879,216 @@ lkv_status lkv_reevict(lkv_ctx* ctx, int64_t n_segments, int32_t head_dim, const
                        int32_t* offsets, void* kp_new, void* vp_new, float* up_new, int32_t* cap_offsets_new,
                        int32_t* lengths_new, int64_t* total_kept, void* stream) {
   if (ctx == nullptr) return LKV_ERR_INVALID_ARG;
-  if (head_dim != lkv::kHeadDim) return fail(ctx, LKV_ERR_UNSUPPORTED, "head_dim must be 128, got %d", head_dim);
-  if (n_segments < 1) return fail(ctx, LKV_ERR_INVALID_ARG, "n_segments = %lld must be >= 1", (long long)n_segments);
-  if (n_segments > kMaxSegments) return fail(ctx, LKV_ERR_UNSUPPORTED, "too many segments");
-  if (cap_offsets == nullptr || lengths == nullptr || lengths_host == nullptr || new_budgets == nullptr ||
-      offsets == nullptr || cap_offsets_new == nullptr || lengths_new == nullptr)
+  if (cap_offsets == nullptr || lengths == nullptr || offsets == nullptr || cap_offsets_new == nullptr || lengths_new == nullptr)
     return fail(ctx, LKV_ERR_INVALID_ARG, "a required pointer is NULL");
-  if (slack < 0) return fail(ctx, LKV_ERR_INVALID_ARG, "slack = %d must be >= 0", slack);
   int64_t total = 0;
   int max_len = 1;
-  for (int64_t i = 0; i < n_segments; ++i) {
-    if (lengths_host[i] < 0) return fail(ctx, LKV_ERR_INVALID_ARG, "length %d of segment %lld is negative", lengths_host[i], (long long)i);
-    if (new_budgets[i] < 0 || new_budgets[i] > lengths_host[i])
-      return fail(ctx, LKV_ERR_INVALID_ARG, "new budget %d of segment %lld is outside [0, %d]", new_budgets[i],
-                  (long long)i, lengths_host[i]);
-    total += new_budgets[i];
-    if (lengths_host[i] > max_len) max_len = lengths_host[i];
-  }
-  if (total + n_segments * slack >= (int64_t)1 << 31)
-    return fail(ctx, LKV_ERR_UNSUPPORTED, "new cache of %lld rows >= 2^31", (long long)(total + n_segments * slack));
+  if (lkv_status st = check_reeviction(ctx, n_segments, head_dim, lengths_host, new_budgets, slack, &total, &max_len)) return st;
   if (total > 0 && (kp == nullptr || vp == nullptr || up == nullptr || idx == nullptr || kp_new == nullptr ||
                     vp_new == nullptr || up_new == nullptr))
     return fail(ctx, LKV_ERR_INVALID_ARG, "a cache, score or index buffer is NULL");
   if (!aligned16(kp) || !aligned16(vp) || !aligned16(kp_new) || !aligned16(vp_new))
     return fail(ctx, LKV_ERR_INVALID_ARG, "kp, vp, kp_new or vp_new is not 16-byte aligned");
-  // tight offsets of the new budgets, the layout the selection writes its indices in
-  if (lkv_status st = lkv_plan_offsets(ctx, n_segments, new_budgets, offsets, nullptr, stream)) return st;
+  if (lkv_status st = reevict_select(ctx, n_segments, new_budgets, max_len, up, cap_offsets, lengths, idx, offsets, stream)) return st;
   hipStream_t st = as_stream(stream);
-  lkv::SeqTable tab;
-  memset(&tab, 0, sizeof(tab));
-  tab.T[0] = max_len;          // upper bound of every segment's length: sizes the LDS region
-  tab.first[0] = 0;
-  tab.first[1] = (int32_t)n_segments;
-  tab.n = 1;
-  lkv::launch_select(tab, nullptr, (int)n_segments, offsets, idx, 0, 0, st, up, cap_offsets, lengths);
-  if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_reevict select launch");
   lkv::launch_compact_regrow(idx, offsets, (int)n_segments, total, slack, kp, vp, up, cap_offsets, lengths, kp_new, vp_new,
                              up_new, st);
   if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_reevict compact launch");
   lkv::launch_grown_layout(offsets, (int)n_segments, slack, cap_offsets_new, lengths_new, st);
   if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_reevict layout launch");
   if (total_kept != nullptr) *total_kept = total;
+  return LKV_OK;
+}
+
+int64_t lkv_quant_scales(int64_t n_segments, int64_t total_rows) {
+  return n_segments > 0 && total_rows >= 0 ? total_rows / lkv::kQuantBlock + n_segments : 0;
+}
+
+lkv_status lkv_compact_quant(lkv_ctx* ctx, const lkv_cache* cache, const float* const* scores, const int32_t* idx,
+                             const int32_t* offsets, int64_t total_kept, int32_t slack, const lkv_quant_rows* packed, float* up,
+                             int32_t* cap_offsets, int32_t* lengths, void* stream) {
+  if (ctx == nullptr) return LKV_ERR_INVALID_ARG;
+  if (lkv_status st = check_cache(ctx, cache, true)) return st;
+  if (offsets == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "offsets is NULL");
+  if (slack < 0) return fail(ctx, LKV_ERR_INVALID_ARG, "slack = %d must be >= 0", slack);
+  if ((cap_offsets == nullptr) != (lengths == nullptr))
+    return fail(ctx, LKV_ERR_INVALID_ARG, "cap_offsets and lengths go together");
+  if (slack > 0 && cap_offsets == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "a cache with slack needs cap_offsets and lengths");
+  if (up != nullptr && scores == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "up needs scores");
+  const int heads = cache->n_layers * cache->n_kv_heads;
+  const int64_t n_seg = (int64_t)heads * cache->n_seq;
+  if (n_seg > kMaxSegments) return fail(ctx, LKV_ERR_UNSUPPORTED, "too many segments");
+  if (total_kept < 0) return fail(ctx, LKV_ERR_INVALID_ARG, "total_kept = %lld must be >= 0", (long long)total_kept);
+  if (lkv_status st = check_quant_total(ctx, total_kept + n_seg * slack)) return st;
+  if (lkv_status st = check_quant_rows(ctx, packed, total_kept, "packed")) return st;
+  if (total_kept > 0 && idx == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "idx is NULL");
+  for (int s = 0; up != nullptr && s < cache->n_seq; ++s)
+    if (scores[s] == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "scores[%d] is NULL", s);
+  hipStream_t st = as_stream(stream);
+  if (cap_offsets != nullptr) {
+    lkv::launch_grown_layout(offsets, (int)n_seg, slack, cap_offsets, lengths, st);
+    if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_compact_quant layout launch");
+  }
+  for (int s0 = 0; s0 < cache->n_seq; s0 += lkv::kMaxSeqPerLaunch) {
+    lkv::SeqTable tab;
+    memset(&tab, 0, sizeof(tab));
+    const int n = cache->n_seq - s0 < lkv::kMaxSeqPerLaunch ? cache->n_seq - s0 : lkv::kMaxSeqPerLaunch;
+    for (int i = 0; i < n; ++i) {
+      tab.k[i] = static_cast<const uint16_t*>(cache->k[s0 + i]);
+      tab.v[i] = static_cast<const uint16_t*>(cache->v[s0 + i]);
+      tab.scores[i] = up != nullptr ? const_cast<float*>(scores[s0 + i]) : nullptr;
+      tab.T[i] = cache->seq_len[s0 + i];
+    }
+    tab.n = n;
+    lkv::launch_quant_compact(tab, packed->format, idx, offsets, (int)n_seg, heads, s0, total_kept, slack, as_quant_rows(packed), up, st);
+    if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_compact_quant launch");
+  }
+  return LKV_OK;
+}
+
+lkv_status lkv_append_quant(lkv_ctx* ctx, int32_t n_seq, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                            const lkv_scorer* scorer, const lkv_rotary* rotary, const int32_t* positions, const void* k_new,
+                            const void* v_new, const lkv_quant_rows* packed, float* up, const int32_t* cap_offsets, int32_t* lengths,
+                            int32_t* overflow, void* stream) {
+  if (ctx == nullptr) return LKV_ERR_INVALID_ARG;
+  if (n_seq < 1 || n_layers < 1 || n_kv_heads < 1) return fail(ctx, LKV_ERR_INVALID_ARG, "n_seq, n_layers and n_kv_heads must be >= 1");
+  if (head_dim != lkv::kHeadDim) return fail(ctx, LKV_ERR_UNSUPPORTED, "head_dim must be 128, got %d", head_dim);
+  const int64_t n_seg = (int64_t)n_seq * n_layers * n_kv_heads;
+  if (n_seg > kMaxSegments) return fail(ctx, LKV_ERR_UNSUPPORTED, "too many segments");
+  if (k_new == nullptr || v_new == nullptr || cap_offsets == nullptr || lengths == nullptr)
+    return fail(ctx, LKV_ERR_INVALID_ARG, "k_new, v_new, cap_offsets or lengths is NULL");
+  if (!aligned16(k_new) || !aligned16(v_new)) return fail(ctx, LKV_ERR_INVALID_ARG, "k_new or v_new is not 16-byte aligned");
+  if (lkv_status st = check_quant_rows(ctx, packed, 1, "packed")) return st;
+  if ((scorer == nullptr) != (up == nullptr)) return fail(ctx, LKV_ERR_INVALID_ARG, "scorer and up go together");
+  lkv::AppendScorer sc = {};
+  if (scorer != nullptr) {
+    if (lkv_status st = check_scorer(ctx, scorer, false)) return st;
+    sc = {static_cast<const uint16_t*>(scorer->w1), scorer->b1, scorer->w2, scorer->b2, scorer->kind == LKV_SCORER_LINEAR ? 0 : 1,
+          scorer->act == LKV_ACT_SILU ? 0 : 1, scorer->hidden, scorer->per_head};
+  }
+  lkv::RotaryArgs rot = {};
+  if (rotary != nullptr) {
+    if (lkv_status st = check_rotary(ctx, rotary)) return st;
+    if (positions == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "rotary needs positions");
+    rot = as_rotary(rotary);
+  }
+  lkv::launch_quant_append(packed->format, (int)n_seg, n_layers * n_kv_heads, n_kv_heads, sc, rotary != nullptr ? &rot : nullptr, positions,
+                           k_new, v_new, as_quant_rows(packed), up, cap_offsets, lengths, overflow, as_stream(stream));
+  if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_append_quant launch");
+  return LKV_OK;
+}
+
+size_t lkv_decode_quant_workspace_bytes(int32_t n_segments, int64_t total_rows, int32_t n_q_heads, int32_t n_kv_heads) {
+  if (n_segments < 0 || total_rows < 0 || n_kv_heads < 1 || n_q_heads < n_kv_heads) return 0;
+  return lkv::quant_decode_workspace_bytes(n_segments, total_rows, n_q_heads / n_kv_heads);
+}
+
+lkv_status lkv_decode_attn_quant(lkv_ctx* ctx, int32_t n_seq, int32_t n_layers, int32_t n_kv_heads, int32_t n_q_heads, int32_t head_dim,
+                                 const void* q, const lkv_quant_rows* packed, const int32_t* cap_offsets, const int32_t* lengths,
+                                 int64_t total_rows, float scale, float* out, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  if (ctx == nullptr) return LKV_ERR_INVALID_ARG;
+  int G = 0;
+  int64_t n_seg = 0;
+  if (lkv_status st = check_decode_geometry(ctx, n_seq, n_layers, n_kv_heads, n_q_heads, head_dim, &G, &n_seg)) return st;
+  if (lkv_status st = check_quant_total(ctx, total_rows)) return st;
+  if (q == nullptr || cap_offsets == nullptr || out == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "q, cap_offsets or out is NULL");
+  if (lkv_status st = check_quant_rows(ctx, packed, total_rows, "packed")) return st;
+  if (!aligned16(q) || !aligned16(out)) return fail(ctx, LKV_ERR_INVALID_ARG, "q or out is not 16-byte aligned");
+  if (!std::isfinite(scale)) return fail(ctx, LKV_ERR_INVALID_ARG, "scale must be finite");
+  const size_t need = lkv::quant_decode_workspace_bytes((int)n_seg, total_rows, G);
+  if (lkv_status st = check_workspace(ctx, workspace, workspace_bytes, need, 256, "decode")) return st;
+  if (hipError_t e = lkv::launch_quant_decode(packed->format, G, q, as_quant_rows(packed), cap_offsets, lengths, (int)n_seg, total_rows, scale,
+                                              out, lse, static_cast<float*>(workspace), as_stream(stream)))
+    return hip_fail(ctx, e, "lkv_decode_attn_quant launch");
+  return LKV_OK;
+}
+
+lkv_status lkv_reevict_quant(lkv_ctx* ctx, int64_t n_segments, int32_t head_dim, const lkv_quant_rows* packed, const float* up,
+                             const int32_t* cap_offsets, const int32_t* lengths, const int32_t* lengths_host,
+                             const int32_t* new_budgets, int32_t slack, int32_t* idx, int32_t* offsets, const lkv_quant_rows* packed_new,
+                             float* up_new, int32_t* cap_offsets_new, int32_t* lengths_new, int64_t* total_kept, void* stream) {
+  if (ctx == nullptr) return LKV_ERR_INVALID_ARG;
+  if (cap_offsets == nullptr || lengths == nullptr || offsets == nullptr || cap_offsets_new == nullptr || lengths_new == nullptr)
+    return fail(ctx, LKV_ERR_INVALID_ARG, "cap_offsets, lengths, offsets, cap_offsets_new or lengths_new is NULL");
+  int64_t total = 0;
+  int max_len = 1;
+  if (lkv_status st = check_reeviction(ctx, n_segments, head_dim, lengths_host, new_budgets, slack, &total, &max_len)) return st;
+  if (lkv_status st = check_quant_rows(ctx, packed, total, "packed")) return st;
+  if (lkv_status st = check_quant_rows(ctx, packed_new, total, "packed_new")) return st;
+  if (packed->format != packed_new->format) return fail(ctx, LKV_ERR_UNSUPPORTED, "packed and packed_new have different formats");
+  if (total > 0 && (up == nullptr || idx == nullptr || up_new == nullptr)) return fail(ctx, LKV_ERR_INVALID_ARG, "up, idx or up_new is NULL");
+  if (lkv_status st = reevict_select(ctx, n_segments, new_budgets, max_len, up, cap_offsets, lengths, idx, offsets, stream)) return st;
+  hipStream_t st = as_stream(stream);
+  lkv::launch_quant_recompact(packed->format, idx, offsets, (int)n_segments, total, slack,
+                              lkv::QuantOld{as_quant_rows(packed), up, cap_offsets, lengths}, as_quant_rows(packed_new), up_new, st);
+  if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_reevict_quant compact launch");
+  lkv::launch_grown_layout(offsets, (int)n_segments, slack, cap_offsets_new, lengths_new, st);
+  if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_reevict_quant layout launch");
+  if (total_kept != nullptr) *total_kept = total;
+  return LKV_OK;
+}
+
+lkv_status lkv_rope(lkv_ctx* ctx, const lkv_rotary* rotary, int32_t dtype, int32_t n_batch, int32_t n_heads, int32_t n_tokens,
+                    int32_t head_dim, const void* x, const int64_t* x_strides, void* y, const int64_t* y_strides,
+                    const int32_t* positions, int64_t positions_stride, int32_t first_position, int32_t backward, void* stream) {
+  if (ctx == nullptr) return LKV_ERR_INVALID_ARG;
+  if (lkv_status st = check_rotary(ctx, rotary)) return st;
+  if (dtype != LKV_BF16 && dtype != LKV_FP32) return fail(ctx, LKV_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (n_batch < 1 || n_heads < 1 || n_tokens < 1) return fail(ctx, LKV_ERR_INVALID_ARG, "n_batch, n_heads and n_tokens must be >= 1");
+  if (head_dim != lkv::kHeadDim) return fail(ctx, LKV_ERR_UNSUPPORTED, "head_dim must be 128, got %d", head_dim);
+  if ((int64_t)n_batch * n_tokens >= (int64_t)1 << 31) return fail(ctx, LKV_ERR_UNSUPPORTED, "n_batch * n_tokens must be below 2^31");
+  if (x == nullptr || y == nullptr || x_strides == nullptr || y_strides == nullptr)
+    return fail(ctx, LKV_ERR_INVALID_ARG, "x, y, x_strides or y_strides is NULL");
+  if (!aligned16(x) || !aligned16(y)) return fail(ctx, LKV_ERR_INVALID_ARG, "x or y is not 16-byte aligned");
+  const int64_t piece = dtype == LKV_FP32 ? 4 : 8;   // elements in 16 bytes
+  for (int i = 0; i < 3; ++i)
+    if (x_strides[i] % piece != 0 || y_strides[i] % piece != 0)
+      return fail(ctx, LKV_ERR_INVALID_ARG, "stride %d of x or y is not a multiple of 16 bytes", i);
+  if (backward != 0 && backward != 1) return fail(ctx, LKV_ERR_INVALID_ARG, "backward must be 0 or 1");
+  if (positions == nullptr && (int64_t)first_position + n_tokens > (int64_t)1 << 31)
+    return fail(ctx, LKV_ERR_INVALID_ARG, "first_position + n_tokens exceeds 2^31");
+  if (x == y)
+    for (int i = 0; i < 3; ++i)
+      if (x_strides[i] != y_strides[i]) return fail(ctx, LKV_ERR_INVALID_ARG, "in place, x and y must have the same strides");
+  const lkv::RopeStrides xs = {x_strides[0], x_strides[1], x_strides[2]}, ys = {y_strides[0], y_strides[1], y_strides[2]};
+  lkv::launch_rope(as_rotary(rotary), dtype == LKV_FP32, x, xs, y, ys, positions, positions_stride, first_position, n_batch, n_heads,
+                   n_tokens, backward != 0, as_stream(stream));
+  if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_rope launch");
+  return LKV_OK;
+}
+
+lkv_status lkv_rope_frequencies(const lkv_rope_scaling* x, double* inv_freq, double* factor) {
+  constexpr double kTwoPi = 6.28318530717958647693;
+  if (x == nullptr || inv_freq == nullptr || factor == nullptr) return LKV_ERR_INVALID_ARG;
+  if (x->rotary_dim < 2 || x->rotary_dim > lkv::kHeadDim || x->rotary_dim % 2 != 0) return LKV_ERR_INVALID_ARG;
+  if (!(x->base > 1.0) || !std::isfinite(x->base)) return LKV_ERR_INVALID_ARG;
+  if (x->kind < LKV_ROPE_PLAIN || x->kind > LKV_ROPE_WAVELENGTHS) return LKV_ERR_INVALID_ARG;
+  if (x->kind != LKV_ROPE_PLAIN && (!(x->stretch >= 1.0) || !std::isfinite(x->stretch))) return LKV_ERR_INVALID_ARG;
+  const bool bands = x->kind == LKV_ROPE_PARTS || x->kind == LKV_ROPE_WAVELENGTHS;
+  if (bands && (!(x->trained_len > 0.0) || !std::isfinite(x->trained_len) || !(x->low > 0.0) || !(x->high > x->low) || !std::isfinite(x->high)))
+    return LKV_ERR_INVALID_ARG;
+  if (x->kind == LKV_ROPE_BASE && x->rotary_dim < 4) return LKV_ERR_INVALID_ARG;
+  const int r = x->rotary_dim;
+  const double s = x->kind == LKV_ROPE_PLAIN ? 1.0 : x->stretch;
+  const double base = x->kind == LKV_ROPE_BASE ? x->base * std::pow(s, (double)r / (r - 2)) : x->base;
+  double first = 0.0, last = 0.0;
+  if (x->kind == LKV_ROPE_PARTS) {
+    // the pair that makes n turns over the trained length: base^(-2 i / r) trained_len = 2 pi n
+    auto pair_of = [&](double turns) { return r * std::log(x->trained_len / (turns * kTwoPi)) / (2.0 * std::log(x->base)); };
+    first = std::max(std::floor(pair_of(x->high)), 0.0);
+    last = std::min(std::ceil(pair_of(x->low)), (double)(r - 1));
+    if (!(last > first)) last = first + 0.001;
+  }
+  for (int i = 0; i < r / 2; ++i) {
+    const double w = std::pow(base, -2.0 * i / r);
+    double keep = 1.0;   // share of the frequency that is not stretched
+    if (x->kind == LKV_ROPE_LINEAR) keep = 0.0;
+    else if (x->kind == LKV_ROPE_PARTS) keep = 1.0 - std::min(std::max((i - first) / (last - first), 0.0), 1.0);
+    else if (x->kind == LKV_ROPE_WAVELENGTHS) keep = std::min(std::max((x->trained_len * w / kTwoPi - x->low) / (x->high - x->low), 0.0), 1.0);
+    inv_freq[i] = w * keep + w / s * (1.0 - keep);
+  }
+  *factor = x->kind == LKV_ROPE_PARTS ? 0.1 * std::log(s) + 1.0 : 1.0;
   return LKV_OK;
 }
 

@@ -2,6 +2,8 @@
 #pragma once
 
 #include "lkv_common.h"
+#include "lkv_quant.h"
+#include "lkv_rotary.h"
 
 namespace lkv {
 
@@ -84,6 +86,44 @@ void launch_masked_attn_bwd(const void* q, const void* k, const void* v, const f
                             const float* lse, const void* d_o, int n_q_heads, int n_kv_heads, int T, float scale,
                             float* dq, float* dk, float* dv, float* dm, float* workspace, size_t workspace_bytes,
                             hipStream_t stream);
+
+// quant_compact.hip
+struct QuantOld {   // the packed 8-bit cache that a re-eviction reads
+  QuantRows rows;
+  const float* up;
+  const int32_t* cap;
+  const int32_t* len;
+};
+void launch_quant_compact(const SeqTable& tab, int format, const int32_t* idx, const int32_t* offsets, int n_segments,
+                          int heads_per_seq, int seq_lo, int64_t total_kept, int slack, const QuantRows& dst, float* up,
+                          hipStream_t stream);
+void launch_quant_recompact(int format, const int32_t* idx, const int32_t* offsets, int n_segments, int64_t total_kept, int slack,
+                            const QuantOld& old, const QuantRows& dst, float* up, hipStream_t stream);
+
+// quant_append.hip
+struct AppendScorer {   // w1 null: no scores
+  const uint16_t* w1;
+  const float* b1;
+  const float* w2;
+  const float* b2;
+  int kind, act, hidden, per_head;
+};
+void launch_quant_append(int format, int n_segments, int heads_per_seq, int n_kv_heads, const AppendScorer& scorer,
+                         const RotaryArgs* rotary, const int32_t* positions, const void* k_new, const void* v_new,
+                         const QuantRows& rows, float* up, const int32_t* cap, int32_t* len, int32_t* overflow, hipStream_t stream);
+
+// quant_decode.hip
+size_t quant_decode_workspace_bytes(int n_segments, int64_t total_rows, int G);
+hipError_t launch_quant_decode(int format, int G, const void* q, const QuantRows& rows, const int32_t* cap, const int32_t* lengths,
+                               int n_segments, int64_t total_rows, float scale, float* out, float* lse, float* ws, hipStream_t stream);
+
+// rope.hip
+struct RopeStrides {   // in elements
+  int64_t batch, head, token;
+};
+void launch_rope(const RotaryArgs& rot, bool f32, const void* x, const RopeStrides& xs, void* y, const RopeStrides& ys,
+                 const int32_t* positions, int64_t positions_stride, int first_position, int n_batch, int n_heads, int n_tokens,
+                 bool backward, hipStream_t stream);
 
 // lkv_h.hip
 int soft_topk_max_n(bool is_f64);

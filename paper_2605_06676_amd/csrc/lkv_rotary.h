@@ -1,0 +1,61 @@
+// Cosines and sines of rotary angles.
+//
+// The angle of position p and frequency w (radians per position) is p w, formed in fp64: at a position of a million an fp32
+// product is off by a sixteenth of a radian, an fp64 one by 1e-10.  It is reduced by multiples of pi / 2 held in two fp64 numbers (two fused
+// multiply-adds) and both functions are their Taylor series on [-pi / 4, pi / 4], whose first terms left out are below
+// 1e-15; results are rounded to fp32 once.  About 25 fp64 operations, without a branch.
+#pragma once
+
+#include "lkv_common.h"
+
+namespace lkv {
+
+struct RotaryArgs {
+  const double* inv_freq;   // [rotary_dim / 2]
+  double factor;            // of cosine and sine
+  int rotary_dim;
+  int pairs;                // 1: channels 2i and 2i + 1 turn together; 0: i and i + rotary_dim / 2
+};
+
+__device__ __forceinline__ void rotary_cos_sin(int position, double inv_freq, double factor, float* c_out, float* s_out) {
+  const double angle = (double)position * inv_freq;
+  constexpr double kTwoOverPi = 0.63661977236758134308;
+  constexpr double kHalfPiHi = 1.57079632679489661923, kHalfPiLo = 6.12323399573676588613e-17;   // pi / 2 and what its fp64 number leaves
+  const double k = rint(angle * kTwoOverPi);
+  double r = fma(-k, kHalfPiHi, angle);
+  r = fma(-k, kHalfPiLo, r);
+  const int quarter = (int)(k - 4.0 * floor(k * 0.25));
+  const double z = r * r;
+  // sin r = r (1 - z / 3! + z^2 / 5! - ...), cos r = 1 - z / 2! + z^2 / 4! - ...
+  double s = -1.0 / 1307674368000.0, c = -1.0 / 87178291200.0;
+  s = fma(s, z, 1.0 / 6227020800.0);
+  c = fma(c, z, 1.0 / 479001600.0);
+  s = fma(s, z, -1.0 / 39916800.0);
+  c = fma(c, z, -1.0 / 3628800.0);
+  s = fma(s, z, 1.0 / 362880.0);
+  c = fma(c, z, 1.0 / 40320.0);
+  s = fma(s, z, -1.0 / 5040.0);
+  c = fma(c, z, -1.0 / 720.0);
+  s = fma(s, z, 1.0 / 120.0);
+  c = fma(c, z, 1.0 / 24.0);
+  s = fma(s, z, -1.0 / 6.0);
+  c = fma(c, z, -0.5);
+  s = fma(s * z, r, r);
+  c = fma(c, z, 1.0);
+  const bool swap = (quarter & 1) != 0;
+  const double cc = swap ? s : c, ss = swap ? c : s;
+  *c_out = (float)((quarter == 1 || quarter == 2 ? -cc : cc) * factor);
+  *s_out = (float)((quarter & 2 ? -ss : ss) * factor);
+}
+
+// (a, b) turned by the angle; each product and sum rounded to fp32 by itself, so that the result does not hang on which of them
+// a compiler fuses.
+__device__ __forceinline__ void rotary_turn(float& a, float& b, float c, float s) {
+#pragma clang fp contract(off)
+  const float y = a * c - b * s;
+  const float z = b * c + a * s;
+  a = y;
+  b = z;
+}
+
+}  // namespace lkv

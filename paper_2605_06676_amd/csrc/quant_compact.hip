@@ -1,0 +1,214 @@
+// Compaction of the kept K/V rows into the packed cache in 8 bits: the gather of compact.hip with a quantisation per 32 rows
+// of a segment on the way (lkv_quant.h has the format).
+//
+// A wave makes one block of 32 rows: its number is the block's scale number, from which a search over the segments' first
+// rows finds the segment.  Sixteen lanes hold a row, 16 bytes each, so that the block's 32 + 32 rows of K and V are sixteen
+// 16-byte loads of every lane, all in flight together, and stay in registers: the largest magnitude is a maximum over them (on
+// the bit patterns, two at a time) and over the lanes, and each piece of 8 values leaves as 8 codes.  The data is
+// read once and written once (512 + 256 bytes a row), which bounds the kernel.
+#include <cstring>
+#include <type_traits>
+
+#include "lkv_kernels.h"
+
+namespace lkv {
+
+constexpr int kQcThreads = 256;
+constexpr int kQcWaves = kQcThreads / 64;
+constexpr int kQcLoads = kQuantBlock / 4;   // rows of a lane
+
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+
+// Largest magnitude of the bf16 values of a piece, as bits, in either half of the result.
+__device__ __forceinline__ uint32_t top2_bf16(const uint4& p, uint32_t so_far) {
+  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+  u16x2_t m = __builtin_bit_cast(u16x2_t, so_far);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, w[i] & 0x7fff7fffu));
+  return __builtin_bit_cast(uint32_t, m);
+}
+
+// The same of the finite ones alone.
+__device__ __forceinline__ uint32_t top2_finite(const uint4& p, uint32_t so_far) {
+  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+  uint32_t lo = so_far & 0xffffu, hi = so_far >> 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = w[i] & 0x7fffu, b = w[i] >> 16 & 0x7fffu;
+    lo = max(lo, a < 0x7f80u ? a : 0u);
+    hi = max(hi, b < 0x7f80u ? b : 0u);
+  }
+  return hi << 16 | lo;
+}
+
+// The block of one side (K or V): from the bf16 pieces of this lane's rows to codes; returns the scale.
+template <int kFormat>
+__device__ __forceinline__ float quant_block_bf16(const uint4 (&x)[kQcLoads], uint2 (&codes)[kQcLoads]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < kQcLoads; ++j) m = top2_bf16(x[j], m);
+  uint32_t top = wave_max_u32(max(m & 0xffffu, m >> 16));
+  const bool wild = top >= 0x7f80u;   // the same in the whole wave
+  if (wild) {
+    m = 0;
+#pragma unroll
+    for (int j = 0; j < kQcLoads; ++j) m = top2_finite(x[j], m);
+    top = wave_max_u32(max(m & 0xffffu, m >> 16));
+  }
+  const float scale = quant_scale<kFormat>(__uint_as_float(top << 16));
+  const float inv = quant_inverse(scale);
+#pragma unroll
+  for (int j = 0; j < kQcLoads; ++j) {
+    float f[8];
+    unpack8(x[j], f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= inv;
+    if (wild) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = quant_tame<kFormat>(f[i]);
+    }
+    codes[j] = make_uint2(quant4<kFormat>(f[0], f[1], f[2], f[3]), quant4<kFormat>(f[4], f[5], f[6], f[7]));
+  }
+  return scale;
+}
+
+// The same from codes with the scales of their old blocks.
+template <int kFormat>
+__device__ __forceinline__ float requant_block(const uint2 (&x)[kQcLoads], const float (&old)[kQcLoads], uint2 (&codes)[kQcLoads]) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < kQcLoads; ++j) {
+    float f[4], g[4];
+    unquant4<kFormat>(x[j].x, f);
+    unquant4<kFormat>(x[j].y, g);
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = fmaxf(fmaxf(m, fabsf(f[i])), fabsf(g[i]));
+    top = fmaxf(top, m * old[j]);
+  }
+  const float scale = quant_scale<kFormat>(__uint_as_float(wave_max_u32(__float_as_uint(top))));
+  const float inv = quant_inverse(scale);
+#pragma unroll
+  for (int j = 0; j < kQcLoads; ++j) {
+    float f[4], g[4];
+    unquant4<kFormat>(x[j].x, f);
+    unquant4<kFormat>(x[j].y, g);
+    const float ratio = old[j] * inv;   // a power of two, at most 256
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[i] *= ratio; g[i] *= ratio; }
+    codes[j] = make_uint2(quant4<kFormat>(f[0], f[1], f[2], f[3]), quant4<kFormat>(g[0], g[1], g[2], g[3]));
+  }
+  return scale;
+}
+
+// kPacked: the rows come from an older packed cache in 8 bits (re-eviction: idx counts rows inside the old segment), else from
+// the prefilled bf16 cache.
+template <int kFormat, bool kPacked>
+__global__ void __launch_bounds__(kQcThreads)
+quant_compact_kernel(SeqTable tab, const int32_t* __restrict__ idx, const int32_t* __restrict__ offsets, int n_segments,
+                     int heads_per_seq, int seq_lo, int slack, QuantRows dst, float* __restrict__ up, QuantOld old) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  auto first_scale = [&](int s) { return quant_first_scale(offsets[s] + slack * s, s); };
+  // the blocks of the sequences that this launch describes
+  const int seg_lo = kPacked ? 0 : seq_lo * heads_per_seq;
+  const int seg_hi = kPacked ? n_segments : min((seq_lo + tab.n) * heads_per_seq, n_segments);
+  const int number = (seg_lo == 0 ? 0 : first_scale(seg_lo)) + (int)blockIdx.x * kQcWaves + wave;
+  const int s = seg_lo + wave_upper_key(seg_hi - seg_lo, number, lane, [&](int i) { return first_scale(seg_lo + i); });
+  const int o = offsets[s], len = offsets[s + 1] - o;
+  const int cap = o + slack * s;
+  const int64_t ahead = (int64_t)(number - quant_first_scale(cap, s)) * kQuantBlock;   // rows of the segment ahead of the block
+  if (ahead >= len) return;   // a number without rows; the whole wave
+  const int first = (int)ahead;
+  const int n = min(len - first, kQuantBlock);
+
+  const int r = lane >> 4, c = lane & 15;
+  int tok = idx[o + first + min(lane & 31, n - 1)];   // of row `lane` of the block; past its last row that row again
+  uint2 kc[kQcLoads], vc[kQcLoads];
+  float ks, vs, u = 0.f;
+  if constexpr (kPacked) {
+    // a row outside the old segment cannot come from the selection; clamped, never followed
+    tok = min(max(tok, 0), max(old.len[s], 1) - 1);
+    const int cap_old = old.cap[s];
+    const int scale0 = quant_first_scale(cap_old, s);
+    uint2 kk[kQcLoads], vv[kQcLoads];
+    float ko[kQcLoads], vo[kQcLoads];
+#pragma unroll
+    for (int j = 0; j < kQcLoads; ++j) {
+      const int t = __shfl(tok, 4 * j + r, 64);
+      const size_t at = ((size_t)cap_old + (size_t)t) * kHeadDim + c * 8;
+      kk[j] = *reinterpret_cast<const uint2*>(old.rows.k + at);
+      vv[j] = *reinterpret_cast<const uint2*>(old.rows.v + at);
+      ko[j] = old.rows.k_scale[scale0 + t / kQuantBlock];
+      vo[j] = old.rows.v_scale[scale0 + t / kQuantBlock];
+    }
+    if (up != nullptr) u = old.up[cap_old + tok];
+    ks = requant_block<kFormat>(kk, ko, kc);
+    vs = requant_block<kFormat>(vv, vo, vc);
+  } else {
+    const int seq = s / heads_per_seq;
+    const int sl = seq - seq_lo;
+    const int T = tab.T[sl];
+    const size_t head = (size_t)(s - seq * heads_per_seq) * (size_t)T;
+    tok = min(max(tok, 0), T - 1);   // clamped, never followed
+    const uint4* k = reinterpret_cast<const uint4*>(tab.k[sl]);
+    const uint4* v = reinterpret_cast<const uint4*>(tab.v[sl]);
+    uint4 kk[kQcLoads], vv[kQcLoads];
+#pragma unroll
+    for (int j = 0; j < kQcLoads; ++j) {
+      const size_t at = (head + (size_t)__shfl(tok, 4 * j + r, 64)) * kChunksPerRow + c;
+      kk[j] = load_stream16(k + at);
+      vv[j] = load_stream16(v + at);
+    }
+    if (up != nullptr) u = tab.scores[sl][head + (size_t)tok];
+    ks = quant_block_bf16<kFormat>(kk, kc);
+    vs = quant_block_bf16<kFormat>(vv, vc);
+  }
+  const size_t row0 = (size_t)cap + (size_t)first;
+#pragma unroll
+  for (int j = 0; j < kQcLoads; ++j) {
+    if (4 * j + r < n) {
+      const size_t at = (row0 + 4 * j + r) * kHeadDim + c * 8;
+      *reinterpret_cast<uint2*>(dst.k + at) = kc[j];
+      *reinterpret_cast<uint2*>(dst.v + at) = vc[j];
+    }
+  }
+  if (up != nullptr && lane < n) up[row0 + lane] = u;
+  if (lane == 0) {
+    dst.k_scale[number] = ks;
+    dst.v_scale[number] = vs;
+  }
+}
+
+template <bool kPacked>
+static void launch_quant_compact_any(const SeqTable& tab, int format, const int32_t* idx, const int32_t* offsets, int n_segments,
+                                     int heads_per_seq, int seq_lo, int64_t total_kept, int slack, const QuantRows& dst, float* up,
+                                     const QuantOld& old, int n_own, hipStream_t stream) {
+  if (total_kept <= 0) return;
+  // block numbers of n_own segments over at most the rows of the whole cache
+  const int64_t numbers = (total_kept + (int64_t)n_segments * slack) / kQuantBlock + n_own + 1;
+  const dim3 grid((unsigned)((numbers + kQcWaves - 1) / kQcWaves));
+  if (format == kQuantE4m3)
+    hipLaunchKernelGGL((quant_compact_kernel<kQuantE4m3, kPacked>), grid, dim3(kQcThreads), 0, stream, tab, idx, offsets, n_segments,
+                       heads_per_seq, seq_lo, slack, dst, up, old);
+  else
+    hipLaunchKernelGGL((quant_compact_kernel<kQuantInt8, kPacked>), grid, dim3(kQcThreads), 0, stream, tab, idx, offsets, n_segments,
+                       heads_per_seq, seq_lo, slack, dst, up, old);
+}
+
+void launch_quant_compact(const SeqTable& tab, int format, const int32_t* idx, const int32_t* offsets, int n_segments,
+                          int heads_per_seq, int seq_lo, int64_t total_kept, int slack, const QuantRows& dst, float* up,
+                          hipStream_t stream) {
+  QuantOld none = {};
+  launch_quant_compact_any<false>(tab, format, idx, offsets, n_segments, heads_per_seq, seq_lo, total_kept, slack, dst, up, none,
+                                  tab.n * heads_per_seq, stream);
+}
+
+void launch_quant_recompact(int format, const int32_t* idx, const int32_t* offsets, int n_segments, int64_t total_kept, int slack,
+                            const QuantOld& old, const QuantRows& dst, float* up, hipStream_t stream) {
+  SeqTable tab;
+  memset(&tab, 0, sizeof(tab));
+  launch_quant_compact_any<true>(tab, format, idx, offsets, n_segments, 1, 0, total_kept, slack, dst, up, old, n_segments, stream);
+}
+
+}  // namespace lkv

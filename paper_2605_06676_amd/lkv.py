@@ -18,6 +18,10 @@ LKV_OK = 0
 SCORER_LINEAR, SCORER_MLP = 0, 1
 ACT_SILU, ACT_GELU_ERF = 0, 1
 POOL_MAX, POOL_AVG = 0, 1
+QUANT_E4M3, QUANT_INT8 = 0, 1
+QUANT_BLOCK = 32
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS, ROPE_WAVELENGTHS = 0, 1, 2, 3, 4
 _STATUS = {0: "LKV_OK", 1: "LKV_ERR_INVALID_ARG", 2: "LKV_ERR_UNSUPPORTED", 3: "LKV_ERR_WORKSPACE", 4: "LKV_ERR_HIP"}
 
 EXPORTS = ("lkv_create", "lkv_destroy", "lkv_last_error", "lkv_version", "lkv_score",
@@ -28,7 +32,9 @@ EXPORTS = ("lkv_create", "lkv_destroy", "lkv_last_error", "lkv_version", "lkv_sc
            "lkv_head_budgets", "lkv_plan_offsets", "lkv_evict_layer", "lkv_compact_grow",
            "lkv_append", "lkv_decode_attn_grown", "lkv_reevict", "lkv_masked_decode_workspace_bytes",
            "lkv_masked_decode_attn", "lkv_masked_attn_forward",
-           "lkv_masked_attn_backward_workspace_bytes", "lkv_masked_attn_backward")
+           "lkv_masked_attn_backward_workspace_bytes", "lkv_masked_attn_backward",
+           "lkv_quant_scales", "lkv_compact_quant", "lkv_append_quant", "lkv_decode_quant_workspace_bytes",
+           "lkv_decode_attn_quant", "lkv_reevict_quant", "lkv_rope_frequencies", "lkv_rope")
 
 
 class LkvError(RuntimeError):
@@ -51,6 +57,19 @@ class _Scorer(C.Structure):
 class _HeadPredictor(C.Structure):
     _fields_ = [("d_e", C.c_int32), ("hidden", C.c_int32), ("w1", C.c_void_p), ("b1", C.c_void_p),
                 ("w2", C.c_void_p), ("b2", C.c_void_p)]
+
+
+class _QuantRows(C.Structure):
+    _fields_ = [("format", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rotary_dim", C.c_int32), ("inv_freq", C.c_void_p), ("factor", C.c_double)]
+
+
+class _RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("rotary_dim", C.c_int32), ("base", C.c_double), ("stretch", C.c_double),
+                ("trained_len", C.c_double), ("low", C.c_double), ("high", C.c_double)]
 
 
 _lib = None
@@ -163,6 +182,28 @@ def load_library() -> C.CDLL:
     lib.lkv_head_budgets.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(_HeadPredictor), C.c_int32, C.c_double,
                                      C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.lkv_head_budgets.restype = C.c_int
+    lib.lkv_quant_scales.argtypes = [C.c_int64, C.c_int64]
+    lib.lkv_quant_scales.restype = C.c_int64
+    lib.lkv_compact_quant.argtypes = [C.c_void_p, C.POINTER(_Cache), C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p, C.c_int64,
+                                      C.c_int32, C.POINTER(_QuantRows), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.lkv_compact_quant.restype = C.c_int
+    lib.lkv_append_quant.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(_Scorer), C.POINTER(_Rotary),
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(_QuantRows)] + [C.c_void_p] * 5
+    lib.lkv_append_quant.restype = C.c_int
+    lib.lkv_decode_quant_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32]
+    lib.lkv_decode_quant_workspace_bytes.restype = C.c_size_t
+    lib.lkv_decode_attn_quant.argtypes = [C.c_void_p] + [C.c_int32] * 5 + [C.c_void_p, C.POINTER(_QuantRows), C.c_void_p, C.c_void_p,
+                                          C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.lkv_decode_attn_quant.restype = C.c_int
+    lib.lkv_reevict_quant.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.POINTER(_QuantRows), C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32, C.c_void_p, C.c_void_p,
+                                      C.POINTER(_QuantRows), C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p]
+    lib.lkv_reevict_quant.restype = C.c_int
+    lib.lkv_rope_frequencies.argtypes = [C.POINTER(_RopeScaling), C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    lib.lkv_rope_frequencies.restype = C.c_int
+    lib.lkv_rope.argtypes = [C.c_void_p, C.POINTER(_Rotary)] + [C.c_int32] * 5 + [C.c_void_p, C.POINTER(C.c_int64), C.c_void_p,
+                             C.POINTER(C.c_int64), C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p]
+    lib.lkv_rope.restype = C.c_int
     _lib = lib
     return lib
 
@@ -550,3 +591,130 @@ def lkv_masked_attn_backward(ctx: Context, q, k, v, m, o, lse, d_o, scale: float
     ctx._check(ctx.lib.lkv_masked_attn_backward(ctx.h, Hq, H, T, d, _ptr(q), _ptr(k), _ptr(v), _ptr(m), _ptr(o),
                                                 _ptr(lse), _ptr(d_o), float(scale), _ptr(dq), _ptr(dk), _ptr(dv),
                                                 _ptr(dm), _ptr(workspace), ws_bytes, _stream_ptr(stream)))
+
+
+class QuantRows:
+    """A packed cache in 8 bits: codes k, v [rows, 128] (torch.float8_e4m3fn or torch.int8, which settles the format) and their
+    fp32 scales, lkv_quant_scales(n_segments, rows) numbers each; contiguous GPU tensors of the caller."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        import torch
+
+        assert k.dtype == v.dtype and k.dtype in (torch.float8_e4m3fn, torch.int8)
+        assert k.dim() == 2 and k.shape[1] == 128 and k.shape == v.shape
+        assert k_scale.dtype == torch.float32 and v_scale.dtype == torch.float32 and k_scale.numel() == v_scale.numel()
+        for t in (k, v, k_scale, v_scale):
+            assert t.is_cuda and t.is_contiguous()
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.rows, self.scales = int(k.shape[0]), int(k_scale.numel())
+        self.c = _QuantRows(QUANT_INT8 if k.dtype == torch.int8 else QUANT_E4M3, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+
+    def _check(self, n_segments: int, rows: int):
+        """What the library cannot see from pointers: that the tensors hold a cache of this size."""
+        assert self.rows >= rows and self.scales >= rows // QUANT_BLOCK + n_segments
+
+
+class Rotary:
+    """A rotation: inv_freq, a GPU fp64 [rotary_dim / 2] tensor of radians per position; pairs: channels 2i and 2i + 1 turn
+    together (else i and i + rotary_dim / 2); factor: of cosine and sine."""
+
+    def __init__(self, inv_freq, pairs: bool = False, factor: float = 1.0):
+        import torch
+
+        assert inv_freq.dtype == torch.float64 and inv_freq.is_cuda and inv_freq.is_contiguous() and inv_freq.dim() == 1
+        self.inv_freq = inv_freq
+        self.c = _Rotary(ROTARY_PAIRS if pairs else ROTARY_HALVES, 2 * inv_freq.numel(), _ptr(inv_freq), float(factor))
+
+
+def lkv_quant_scales(n_segments: int, total_rows: int) -> int:
+    return int(load_library().lkv_quant_scales(int(n_segments), int(total_rows)))
+
+
+def lkv_compact_quant(ctx: Context, cache: Cache, idx, offsets, total_kept: int, packed: QuantRows, slack: int = 0,
+                      scores: Optional[Sequence] = None, up=None, cap_offsets=None, lengths=None, stream=None) -> None:
+    """lkv_compact (slack 0) or lkv_compact_grow into a packed 8-bit cache of total_kept + n_segments * slack rows."""
+    packed._check(cache.n_segments, int(total_kept) + cache.n_segments * slack)
+    sp = None if scores is None else (C.c_void_p * cache.n_seq)(*[s.data_ptr() for s in scores])
+    ctx._check(ctx.lib.lkv_compact_quant(ctx.h, C.byref(cache.c), sp, _ptr(idx), _ptr(offsets), int(total_kept), int(slack),
+                                         C.byref(packed.c), _ptr(up), _ptr(cap_offsets), _ptr(lengths), _stream_ptr(stream)))
+
+
+def lkv_append_quant(ctx: Context, n_seq: int, L: int, H: int, d: int, k_new, v_new, packed: QuantRows, cap_offsets, lengths,
+                     scorer: Optional[dict] = None, up=None, rotary: Optional[Rotary] = None, positions=None, overflow=None,
+                     stream=None) -> None:
+    """k_new, v_new: bf16 [n_seq, L, H, 128]; positions: GPU int32 [n_seq] with rotary; scorer and up: both or neither."""
+    import torch
+
+    assert all(t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == n_seq * L * H * d for t in (k_new, v_new))
+    assert positions is None or (positions.dtype == torch.int32 and positions.numel() == n_seq and positions.is_contiguous())
+    sc = None if scorer is None else C.byref(_scorer_struct(scorer))
+    ctx._check(ctx.lib.lkv_append_quant(ctx.h, n_seq, L, H, d, sc, None if rotary is None else C.byref(rotary.c), _ptr(positions),
+                                        _ptr(k_new), _ptr(v_new), C.byref(packed.c), _ptr(up), _ptr(cap_offsets), _ptr(lengths),
+                                        _ptr(overflow), _stream_ptr(stream)))
+
+
+def lkv_decode_quant_workspace_bytes(n_segments: int, total_rows: int, n_q_heads: int, n_kv_heads: int) -> int:
+    return int(load_library().lkv_decode_quant_workspace_bytes(n_segments, int(total_rows), n_q_heads, n_kv_heads))
+
+
+def lkv_decode_attn_quant(ctx: Context, n_seq: int, L: int, H: int, Hq: int, d: int, q, packed: QuantRows, cap_offsets, lengths,
+                          total_rows: int, scale: float, out, lse, workspace, stream=None) -> None:
+    """lkv_decode_attn (lengths None) or lkv_decode_attn_grown over a packed 8-bit cache of total_rows rows."""
+    packed._check(n_seq * L * H, int(total_rows))
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ctx._check(ctx.lib.lkv_decode_attn_quant(ctx.h, n_seq, L, H, Hq, d, _ptr(q), C.byref(packed.c), _ptr(cap_offsets), _ptr(lengths),
+                                             int(total_rows), float(scale), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes,
+                                             _stream_ptr(stream)))
+
+
+def lkv_reevict_quant(ctx: Context, d: int, packed: QuantRows, up, cap_offsets, lengths, lengths_host, new_budgets, slack: int, idx,
+                      offsets, packed_new: QuantRows, up_new, cap_offsets_new, lengths_new, stream=None) -> int:
+    """Shrinks a packed 8-bit cache with slack to new_budgets (host int32 [n_segments]) and returns the rows kept."""
+    import numpy as np
+
+    lh = np.ascontiguousarray(np.asarray(lengths_host, dtype=np.int32).reshape(-1))
+    nb = np.ascontiguousarray(np.asarray(new_budgets, dtype=np.int32).reshape(-1))
+    assert lh.size == nb.size
+    packed_new._check(nb.size, int(nb.sum(dtype=np.int64)) + nb.size * slack)
+    total = C.c_int64(0)
+    ctx._check(ctx.lib.lkv_reevict_quant(ctx.h, lh.size, d, C.byref(packed.c), _ptr(up), _ptr(cap_offsets), _ptr(lengths),
+                                         lh.ctypes.data_as(C.POINTER(C.c_int32)), nb.ctypes.data_as(C.POINTER(C.c_int32)), int(slack),
+                                         _ptr(idx), _ptr(offsets), C.byref(packed_new.c), _ptr(up_new), _ptr(cap_offsets_new),
+                                         _ptr(lengths_new), C.byref(total), _stream_ptr(stream)))
+    return int(total.value)
+
+
+def lkv_rope_frequencies(kind: int, rotary_dim: int, base: float, stretch: float = 1.0, trained_len: float = 0.0, low: float = 0.0,
+                         high: float = 0.0):
+    """Frequencies (host fp64 array [rotary_dim / 2], radians per position) and factor of a context extension."""
+    import numpy as np
+
+    freq = np.empty(max(int(rotary_dim), 2) // 2, dtype=np.float64)
+    factor = C.c_double(0.0)
+    x = _RopeScaling(int(kind), int(rotary_dim), float(base), float(stretch), float(trained_len), float(low), float(high))
+    st = load_library().lkv_rope_frequencies(C.byref(x), freq.ctypes.data_as(C.POINTER(C.c_double)), C.byref(factor))
+    if st != LKV_OK:
+        raise LkvError(st, "lkv_rope_frequencies: an argument is out of range")
+    return freq, factor.value
+
+
+def lkv_rope(ctx: Context, rotary: Rotary, x, y, positions=None, first_position: int = 0, backward: bool = False, stream=None) -> None:
+    """x, y: bf16 or fp32 [batch, heads, tokens, 128] (or without the batch), of any strides with the channels contiguous; y may
+    be x.  positions: GPU int32 [batch, tokens], or [tokens] for all batches, or None: first_position + t."""
+    import torch
+
+    assert x.shape == y.shape and x.dtype == y.dtype and x.dtype in (torch.bfloat16, torch.float32) and x.dim() in (3, 4)
+    assert x.is_cuda and y.is_cuda and x.stride(-1) == 1 and y.stride(-1) == 1
+    B, Hn, T, d = x.shape if x.dim() == 4 else (1, *x.shape)
+
+    def strides(t):   # of a single batch, head or token: never followed
+        s = t.stride()[:-1] if t.dim() == 4 else (0, *t.stride()[:-1])
+        return (C.c_int64 * 3)(*[0 if n == 1 else st for n, st in zip((B, Hn, T), s)])
+
+    step = 0
+    if positions is not None:
+        assert positions.dtype == torch.int32 and positions.is_cuda and positions.shape[-1] == T and (T == 1 or positions.stride(-1) == 1)
+        assert positions.dim() == 1 or positions.shape == (B, T)
+        step = positions.stride(0) if positions.dim() == 2 and B > 1 else 0
+    ctx._check(ctx.lib.lkv_rope(ctx.h, C.byref(rotary.c), 1 if x.dtype == torch.float32 else 0, B, Hn, T, d, _ptr(x), strides(x),
+                                _ptr(y), strides(y), _ptr(positions), step, int(first_position), int(backward), _stream_ptr(stream)))

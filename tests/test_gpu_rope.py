@@ -1,0 +1,215 @@
+"""Rotary positions on the GPU against the 64-bit oracle.
+
+Tolerance.  The cosine and sine are right to half an fp32 step (2^-24 of at most |factor|), two products and a sum round at
+2^-24 each: |y - ref| <= 4 * 2^-24 * |factor| (|x_a| + |x_b|), and a bf16 result is off by half its step more, 2^-9 of
+itself (2^-8 relative covers a value just above a power of two whose fp32 error moved it over).  The angle is an fp64 product, off by
+2^-53 of itself; at 2^31 radians that is 2.4e-7, counted with the factor 2 (|x_a| + |x_b|)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rotary as R
+from paper_2605_06676_amd import lkv
+
+pytestmark = pytest.mark.gpu
+
+KIND = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = lkv.Context(0)
+    yield c
+    c.close()
+
+
+def _rotary(r, pairs, factor=1.0, base=10000.0):
+    w = base ** (-np.arange(0, r, 2) / r)
+    return w, lkv.Rotary(torch.from_numpy(w).cuda(), pairs=pairs, factor=factor)
+
+
+def _assert_close(y, x, positions, w, factor, pairs, backward):
+    r = 2 * w.size
+    bits = torch.int16 if x.dtype == torch.bfloat16 else torch.int32
+    assert torch.equal(y.contiguous().view(bits)[..., r:], x.contiguous().view(bits)[..., r:])   # bit for bit
+    x64, y64 = x.double().cpu().numpy(), y.double().cpu().numpy()
+    ref = R.rotate(x64, positions, w, factor, pairs, backward)
+    a, b = R.channels(r, pairs)
+    size = np.abs(x64[..., a]) + np.abs(x64[..., b])
+    far = np.abs(np.asarray(positions, dtype=np.float64)).max() * w.max() * 2.0 ** -52
+    tol = (4 * 2.0 ** -24 + far) * abs(factor) * size + 2.0 ** -140
+    for ch in (a, b):
+        t = tol + (2.0 ** -8 * np.abs(ref[..., ch]) + 2.0 ** -134 if x.dtype == torch.bfloat16 else 0)
+        assert (np.abs(y64[..., ch] - ref[..., ch]) <= t).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("r", [2, 16, 34, 48, 64, 96, 128])
+@pytest.mark.parametrize("backward", [False, True])
+def test_rotation(ctx, kind, pairs, r, backward):
+    rng = np.random.default_rng(r)
+    B, H, T = 2, 5, 19
+    x = torch.from_numpy(rng.normal(size=(B, H, T, 128)) * 3).to(KIND[kind]).cuda()
+    y = torch.full_like(x, float("nan"))
+    pos = rng.integers(0, 100000, (B, T))
+    w, rot = _rotary(r, pairs, 1.25)
+    lkv.lkv_rope(ctx, rot, x, y, positions=torch.from_numpy(pos).int().cuda(), backward=backward)
+    _assert_close(y, x, pos[:, None, :], w, 1.25, pairs, backward)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("B,H,T", [(1, 1, 1), (1, 33, 1), (9, 4, 1), (1, 3, 8), (1, 2, 1000), (300, 1, 3), (1, 70, 9), (64, 40, 1)])
+def test_sizes_and_positions_counted_from_the_first(ctx, kind, B, H, T):
+    x = torch.randn((B, H, T, 128), generator=torch.Generator().manual_seed(T)).to(KIND[kind]).cuda()
+    y = torch.full_like(x, float("nan"))
+    w, rot = _rotary(128, False)
+    lkv.lkv_rope(ctx, rot, x, y, first_position=777)
+    _assert_close(y, x, 777 + np.arange(T), w, 1.0, False, False)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("r", [128, 34])
+def test_strides_in_place_and_other_streams(ctx, kind, r):
+    g = torch.Generator().manual_seed(1)
+    pos = torch.randint(0, 5000, (13,), generator=g)
+    w, rot = _rotary(r, True)
+    # [batch, tokens, heads, channels] in memory, and a slice of a wider tensor
+    wide = torch.randn((2, 13, 7 + 2, 128), generator=g).to(KIND[kind]).cuda()
+    before = wide.clone()
+    x = wide[:, :, 1:8].transpose(1, 2)
+    y = torch.empty((7, 2, 13, 128), dtype=KIND[kind], device="cuda").transpose(0, 1)
+    lkv.lkv_rope(ctx, rot, x, y, positions=pos.int().cuda())                     # one row of positions for all batches
+    _assert_close(y, x, pos.numpy(), w, 1.0, True, False)
+    assert torch.equal(wide, before)
+    want = y.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    lkv.lkv_rope(ctx, rot, x, x, positions=pos.int().cuda(), stream=side)
+    side.synchronize()
+    assert torch.equal(x, want) and torch.equal(wide[:, :, 0], before[:, :, 0]) and torch.equal(wide[:, :, 8], before[:, :, 8])
+    # three dimensions: [heads, tokens, channels], as the attention takes them
+    a = torch.randn((3, 13, 128), generator=g).to(KIND[kind]).cuda()
+    b = torch.empty_like(a)
+    lkv.lkv_rope(ctx, rot, a, b, positions=pos.int().cuda())
+    _assert_close(b, a, pos.numpy(), w, 1.0, True, False)
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_far_and_negative_positions(ctx, pairs):
+    pos = np.array([0, -1, -2 ** 31, 2 ** 31 - 1, 1 << 20, 123456789, 7, -99999])
+    x = torch.randn((1, 2, 8, 128), generator=torch.Generator().manual_seed(2)).cuda()
+    y = torch.empty_like(x)
+    w, rot = _rotary(128, pairs, base=500000.0)
+    lkv.lkv_rope(ctx, rot, x, y, positions=torch.from_numpy(pos).int().cuda()[None])
+    _assert_close(y, x, pos, w, 1.0, pairs, False)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("r", [64, 34])
+def test_channels_behind_the_rotated_ones_are_copied_whatever_they_hold(ctx, kind, r):
+    bits = torch.int16 if kind == "bf16" else torch.int32
+    info = torch.iinfo(bits)
+    x = torch.randint(info.min, info.max, (1, 2, 5, 128), generator=torch.Generator().manual_seed(3), dtype=bits).cuda()
+    x[..., :r] = 0
+    y = torch.zeros_like(x)
+    for pairs in (False, True):
+        lkv.lkv_rope(ctx, _rotary(r, pairs)[1], x.view(KIND[kind]), y.view(KIND[kind]), first_position=3)
+        assert torch.equal(x[..., r:], y[..., r:])
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_gradient_against_differences_and_the_attention_it_feeds(ctx, pairs):
+    """Forward: rotated q and k in bf16 to the masked attention; backward: its fp32 gradients through the transposed rotation."""
+    H, Hq, T = 2, 4, 77
+    g = torch.Generator().manual_seed(4)
+    w, rot = _rotary(96, pairs, 1.1)
+    x = {n: torch.randn((h, T, 128), generator=g).to(torch.bfloat16).cuda() for n, h in (("q", Hq), ("k", H), ("v", H))}
+    m = torch.rand((H, T), generator=g).cuda()
+    m[:, 0] = 1.0
+    d_o = torch.randn((Hq, T, 128), generator=g).to(torch.bfloat16).cuda()
+    y = {n: torch.empty_like(x[n]) for n in ("q", "k")}
+    for n in y:
+        lkv.lkv_rope(ctx, rot, x[n], y[n])
+    f = dict(device="cuda", dtype=torch.float32)
+    o, lse = torch.empty((Hq, T, 128), **f), torch.empty((Hq, T), **f)
+    lkv.lkv_masked_attn_forward(ctx, y["q"], y["k"], x["v"], m, 128 ** -0.5, o, lse)
+    dq, dk, dv, dm = torch.empty((Hq, T, 128), **f), torch.empty((H, T, 128), **f), torch.empty((H, T, 128), **f), torch.empty((H, T), **f)
+    ws = torch.empty(lkv.lkv_masked_attn_backward_workspace_bytes(Hq, H, T), dtype=torch.uint8, device="cuda")
+    lkv.lkv_masked_attn_backward(ctx, y["q"], y["k"], x["v"], m, o, lse, d_o, 128 ** -0.5, dq, dk, dv, dm, ws)
+    got = {}
+    for n, d in (("q", dq), ("k", dk)):
+        got[n] = torch.empty_like(d)
+        lkv.lkv_rope(ctx, rot, d, got[n], backward=True)
+        _assert_close(got[n], d, np.arange(T), w, 1.1, pairs, True)
+
+    # the whole chain in fp64: autograd of the same formulas at the same inputs
+    a, b = (torch.from_numpy(c) for c in R.channels(96, pairs))
+    ang = torch.arange(T, dtype=torch.float64)[:, None] * torch.from_numpy(w)
+    c, s = 1.1 * torch.cos(ang), 1.1 * torch.sin(ang)
+
+    def turn(t):
+        z = t.clone()
+        z[..., a], z[..., b] = t[..., a] * c - t[..., b] * s, t[..., a] * s + t[..., b] * c
+        return z
+
+    def loss(q, k):
+        sc = (turn(q).reshape(H, Hq // H, T, 128) @ turn(k)[:, None].transpose(-1, -2)) * 128 ** -0.5
+        e = torch.exp(sc - sc.amax(-1, keepdim=True)) * m.double().cpu()[:, None, None] * torch.tril(torch.ones(T, T, dtype=torch.float64))
+        out = (e / e.sum(-1, keepdim=True)) @ x["v"].double().cpu()[:, None]
+        return (out.reshape(Hq, T, 128) * d_o.double().cpu()).sum()
+
+    q64, k64 = (x[n].double().cpu().requires_grad_(True) for n in ("q", "k"))
+    loss(q64, k64).backward()
+    for n, ref in (("q", q64.grad), ("k", k64.grad)):
+        # rotated q and k are rounded to bf16 (half a step, 2^-9 relative, at most 2^-8), the attention's backward has bf16 products
+        # of its own: the relative error of the whole gradient stays below 2^-5
+        assert (got[n].double().cpu() - ref).norm() <= 2.0 ** -5 * ref.norm()
+    # differences of the fp64 loss along two directions
+    for seed in (5, 6):
+        u = torch.randn(q64.shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+        h = 1e-6
+        with torch.no_grad():
+            diff = (loss(q64 + h * u, k64) - loss(q64 - h * u, k64)) / (2 * h)
+        assert abs((q64.grad * u).sum() - diff) <= 1e-6 * q64.grad.norm() * u.norm()
+        assert abs((got["q"].double().cpu() * u).sum() - diff) <= 2.0 ** -5 * q64.grad.norm() * u.norm()
+
+
+def test_a_forward_and_a_backward_rotation_give_the_tensor_back(ctx):
+    x = torch.randn((1, 3, 50, 128), generator=torch.Generator().manual_seed(7)).cuda()
+    y = x.clone()
+    rot = _rotary(128, False)[1]
+    lkv.lkv_rope(ctx, rot, y, y, first_position=12345)
+    assert not torch.equal(x, y)
+    lkv.lkv_rope(ctx, rot, y, y, first_position=12345, backward=True)
+    assert (x - y).abs().max() <= 16 * 2.0 ** -24 * x.abs().max()
+
+
+def test_refusals(ctx):
+    import ctypes as C
+
+    x = torch.zeros((2, 3, 4, 128), dtype=torch.bfloat16, device="cuda")
+    y = torch.full_like(x, 5.0)
+    rot = _rotary(64, False)[1]
+    ptr = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+    good = (C.c_int64 * 3)(3 * 4 * 128, 4 * 128, 128)
+
+    def call(want, rotary=rot.c, dtype=0, n=(2, 3, 4), d=128, a=ptr(x), xs=good, b=ptr(y), ys=good, first=0, backward=0):
+        st = ctx.lib.lkv_rope(ctx.h, None if rotary is None else C.byref(rotary), dtype, *n, d, a, xs, b, ys, None, 0, first, backward, None)
+        assert st == want, ctx.lib.lkv_last_error(ctx.h)
+
+    odd = lambda i, v: (C.c_int64 * 3)(*[v if j == i else s for j, s in enumerate(good)])  # noqa: E731
+    bad = lambda **kw: lkv._Rotary(**{**dict(layout=0, rotary_dim=64, inv_freq=rot.c.inv_freq, factor=1.0), **kw})  # noqa: E731
+    call(1, rotary=None); call(1, dtype=2); call(1, n=(0, 3, 4)); call(1, n=(2, -3, 4)); call(1, n=(2, 3, 0)); call(2, d=64)
+    call(1, a=None); call(1, b=None); call(1, xs=None); call(1, ys=None); call(1, a=C.c_void_p(x.data_ptr() + 2)); call(1, b=C.c_void_p(y.data_ptr() + 8))
+    for i in range(3):
+        call(1, xs=odd(i, 132)); call(1, ys=odd(i, 4))
+    call(1, b=ptr(x), ys=odd(2, 256)); call(1, backward=2); call(1, first=2 ** 31 - 2); call(2, n=(1 << 16, 1, 1 << 15))
+    call(1, rotary=bad(layout=3)); call(1, rotary=bad(rotary_dim=0)); call(1, rotary=bad(rotary_dim=7)); call(1, rotary=bad(rotary_dim=256))
+    call(1, rotary=bad(inv_freq=None)); call(1, rotary=bad(factor=float("inf")))
+    with pytest.raises(AssertionError):
+        lkv.lkv_rope(ctx, rot, x.transpose(2, 3), y.transpose(2, 3))
+    with pytest.raises(AssertionError):
+        lkv.lkv_rope(ctx, rot, x, y, positions=torch.zeros((2, 3), dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert (y == 5).all()
