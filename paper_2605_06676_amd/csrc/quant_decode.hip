@@ -1,22 +1,31 @@
 // One decode step of grouped-query attention over the packed cache in 8 bits (lkv_quant.h): decode.hip's operator with half the
 // bytes per row.
 //
-// Work decomposition.  A chunk is up to C rows of one segment, C a multiple of the 32 rows of a scale; chunk j of segment s has number
-// cap[s] / C + s + j, which orders them as scale numbers order the blocks, so that a wave finds its segment by a search over
-// the segments' first rows and no table has to be made.  A segment always has its number of chunk 0, where an empty one gets its
-// zeros.  The four waves of a block take the chunk's tiles of 32 rows in turn and merge their running maximum, denominator and sums in LDS; a
-// segment of one chunk is finished there, the others leave partials, numbered as the chunks, to a second kernel.
+// Work decomposition.  The scale numbers count the tiles of 32 rows through all segments, so they are a flat list of equal work: wave
+// w takes numbers [w n, (w + 1) n), whatever segments they belong to, and n is chosen so that the launch is one round of resident
+// waves.  A search over the segments' first numbers finds where a wave starts; from there it walks from segment to segment, and
+// the rows of a segment in its range are a piece.  A piece that is a whole segment is finished by its wave; other pieces go to workspace slot
+// (wave + segment), which is a slot of their own because both grow along the rows, except that the four waves of a block that
+// lies inside one segment merge their pieces in LDS into one.  A second kernel merges the slots of each segment.  A segment always has a number, where an
+// empty one gets its zeros.
+// (Chunks of a segment's rows dealt to blocks, a power of two of rows each, left a third of the waves idle: 256 segments of 1.26
+// million rows 71.7 us with the best chunk, 105.5 with twice as many rows in it.)
 //
-// Arithmetic.  Both products run on the matrix cores in bf16, into which every code converts exactly; the scales never touch
-// the operands: the keys' scale multiplies the scores, the values' scale the probabilities.
-//   S^T[token, head] = K[token, :] . Q[head, :]^T      (A = K tile, B = Q^T)
-//   O[head, ch]     += P[head, token] V[token, ch]     (A = P,      B = V tile)
+// Arithmetic.  Both products run on the matrix cores; the scales never touch the operands: the keys' scale multiplies the scores,
+// the values' scale the probabilities.
+//   S^T[token, head] = K[token, :] . Q[head, :]^T      (A = K tile, B = Q^T; bf16, into which every code converts exactly)
+//   O[head, ch]     += P[head, token] V[token, ch]     (A = P,      B = V tile; f16, likewise)
 // Nothing is staged in LDS.  The first product's operand needs 8 channels of a token in a lane: a sum over channels may
 // take them in any order, so a lane takes 16 contiguous bytes of its token's row for two steps and Q's operand is read in that
 // order.  The second needs 8 tokens of a channel in a lane: it loads 8 bytes, 8 channels, of each of the 8 tokens whose scores the
-// first product left with it, and turns the 8 x 8 bytes about with byte permutes (32 for a tile); column c of the m-th
-// product then is channel 8 c + m, and a lane ends with 8 contiguous channels of the output.  Softmax runs in fp32 in the
-// log2 domain; P is rounded to bf16 and what the rounding left is multiplied too, as in decode.hip.
+// first product left with it, and byte permutes (16 for a tile) put the same channel of two tokens side by side, which convert
+// together; column c of the m-th product then is channel 8 c + m, and a lane ends with 8 contiguous channels of the output.
+// Softmax runs in fp32 in the log2 domain.  The weights of the values' codes are at most 1, since the sums are kept in units of the
+// largest value scale so far; they are rounded to f16 and what that left is multiplied too, which holds 22 bits of them
+// (error of the output against 64 bits 2e-7; with two bf16 parts, 16 bits, it was 1.1e-6).
+//
+// Bound by the stream of the rows: 1.26 million rows of 256 segments 56 us (5.8 TB/s) and 5 us for the merge; 2.9 million of
+// 896 in int8 131 us (5.75 TB/s).
 #include <type_traits>
 
 #include "lkv_kernels.h"
@@ -26,19 +35,24 @@ namespace lkv {
 constexpr int kQdThreads = 256;
 constexpr int kQdWaves = kQdThreads / 64;
 constexpr int kQdTile = kQuantBlock;
-constexpr int kQdMinChunk = 128;        // rows: a tile for every wave
-constexpr int kQdTargetChunks = 1024;   // chunks that a launch wants
-constexpr int kQdMergeThreads = kHeadDim;
+// Waves on a SIMD, and the blocks of a full launch (one round of resident ones).  Two hide the loads' latency, since the next
+// tile's are always on their way; three bring more pieces to merge, and four leave too few registers (256 segments of 1.26
+// million rows 64.1 : 64.7 : 85.7 us, 896 of 2.9 million 143.6 : 148.9 : 180.0).
+constexpr int kQdWavesPerSimd = 2;
+constexpr int kQdBlocks = 512;
+constexpr int kQdManyPieces = 4;        // blocks a segment from which a block of the merge has one query head
 constexpr float kQdLog2e = 1.4426950408889634f;
 constexpr float kQdLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float qd_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2_t;
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
-// Eight codes to bf16, exact.
+// Eight codes of a key to bf16, exact.
 template <int kFormat>
-__device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t lo, uint32_t hi) {
+__device__ __forceinline__ bf16x8_t key_operand(uint32_t lo, uint32_t hi) {
   uint4 w;
   if constexpr (kFormat == kQuantE4m3) {
     w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
@@ -57,128 +71,191 @@ __device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t lo, uint32_t hi) {
   return __builtin_bit_cast(bf16x8_t, w);
 }
 
-// Bytes of four rows turned about: out[b] holds byte b of a, b, c and d.
-__device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t (&out)[4]) {
-  const uint32_t ab_lo = __builtin_amdgcn_perm(b, a, 0x05010400u), ab_hi = __builtin_amdgcn_perm(b, a, 0x07030602u);
-  const uint32_t cd_lo = __builtin_amdgcn_perm(d, c, 0x05010400u), cd_hi = __builtin_amdgcn_perm(d, c, 0x07030602u);
-  out[0] = __builtin_amdgcn_perm(cd_lo, ab_lo, 0x05040100u);
-  out[1] = __builtin_amdgcn_perm(cd_lo, ab_lo, 0x07060302u);
-  out[2] = __builtin_amdgcn_perm(cd_hi, ab_hi, 0x05040100u);
-  out[3] = __builtin_amdgcn_perm(cd_hi, ab_hi, 0x07060302u);
+// Two codes, the low or high half of w, to f16, exact.
+template <int kFormat, bool kHigh>
+__device__ __forceinline__ uint32_t two_values(uint32_t w) {
+  if constexpr (kFormat == kQuantE4m3) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, kHigh));
+  } else {
+    // w holds code + 128: under the exponent of 1024 that is the f16 number 1152 + code
+    const uint32_t biased = __builtin_amdgcn_perm(0x64646464u, w, kHigh ? 0x04030402u : 0x04010400u);
+    const f16x2_t v = __builtin_bit_cast(f16x2_t, biased) - f16x2_t{(_Float16)1152.f, (_Float16)1152.f};
+    return __builtin_bit_cast(uint32_t, v);
+  }
 }
 
-// What a lane holds of a tile of 32 rows, and the tile's scales.
-struct QdTile {
-  uint4 k[2][2];   // [16-token half][64-channel half]: token 16 h + c, bytes 64 w + 16 r .. + 15
-  uint2 v[2][4];   // token 16 h + 4 r + e, bytes 8 c .. 8 c + 7
-  float ks, vs;
+// The part of a segment that a wave has.
+struct QdPiece {
+  int s;               // -1: none
+  int tile, end;       // its tiles, counted from the segment's first row
+  int len;             // rows of the segment
+  int cap;             // its first row
 };
 
 template <int kFormat>
-__global__ void __launch_bounds__(kQdThreads)
+__global__ void __launch_bounds__(kQdThreads, kQdWavesPerSimd)
 quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_t* __restrict__ cap,
-                    const int32_t* __restrict__ lengths /* rows in use, or null: all of them */, int n_segments, int chunk_rows, int G,
-                    float scale, float* __restrict__ out, float* __restrict__ lse, float* __restrict__ ws_acc,
+                    const int32_t* __restrict__ lengths /* rows in use, or null: all of them */, int n_segments, int n_numbers,
+                    int per_wave, int G, float scale, float* __restrict__ out, float* __restrict__ lse, float* __restrict__ ws_acc,
                     float* __restrict__ ws_m, float* __restrict__ ws_l) {
   extern __shared__ __align__(16) float merge_lds[];   // [waves][G][128] sums, then [waves][G] maxima, then denominators
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane >> 4, c = lane & 15;
-  const int number = blockIdx.x;
-  auto first_chunk = [&](int s) { return cap[s] / chunk_rows + s; };
-  const int s = wave_upper_key(n_segments, number, lane, first_chunk);
-  const int lo = cap[s];
-  const int len = max(lengths != nullptr ? lengths[s] : cap[s + 1] - lo, 0);
-  const int64_t ahead = (int64_t)(number - first_chunk(s)) * chunk_rows;   // rows of the segment ahead of this chunk
-  if (ahead >= len) {
-    if (ahead == 0) {   // an empty segment: zero output, lse = -inf
-      for (int o = tid; o < G * kHeadDim; o += kQdThreads) out[(size_t)s * G * kHeadDim + o] = 0.f;
-      if (lse != nullptr && tid < G) lse[(size_t)s * G + tid] = -INFINITY;
-    }
-    return;
-  }
-  const int n_rows = (int)min((int64_t)chunk_rows, len - ahead);
-  const int n_tiles = (n_rows + kQdTile - 1) / kQdTile;
-  const int64_t row0 = (int64_t)lo + ahead;
-  const int scale0 = quant_first_scale(lo, s) + (int)(ahead / kQuantBlock);
-  const uint8_t* kbase = rows.k + row0 * kHeadDim;
-  const uint8_t* vbase = rows.v + row0 * kHeadDim;
+  const int wave_id = blockIdx.x * kQdWaves + wave;
+  const int from = min(wave_id * per_wave, n_numbers), to = min(from + per_wave, n_numbers);
+  if (from >= to) return;   // behind the last number; such a block lies inside no segment
 
-  auto load_tile = [&](QdTile& x, int t) __attribute__((always_inline)) {
-    const int last = n_rows - 1;
+  auto segment = [&](int s) __attribute__((always_inline)) {   // its part of this wave
+    QdPiece x;
+    x.s = s;
+    x.cap = __builtin_amdgcn_readfirstlane(cap[s]);   // the same in all lanes: kept in scalar registers
+    x.len = __builtin_amdgcn_readfirstlane(max(lengths != nullptr ? lengths[s] : cap[s + 1] - x.cap, 0));
+    const int first = quant_first_scale(x.cap, s);
+    x.tile = max(from - first, 0);
+    x.end = min(to - first, (x.len + kQdTile - 1) / kQdTile);
+    if (first >= to) x.s = -1;
+    return x;
+  };
+  // The next piece with rows; empty segments on the way get their zeros, from the wave that has their number.
+  auto next_piece = [&](int s) __attribute__((always_inline)) {
+    for (;;) {
+      if (s >= n_segments) return QdPiece{-1, 0, 0, 0, 0};
+      const QdPiece x = segment(s);
+      if (x.s < 0 || x.tile < x.end) return x;
+      if (x.len == 0 && quant_first_scale(x.cap, s) >= from) {
+        for (int o = lane; o < G * kHeadDim; o += 64) out[(size_t)s * G * kHeadDim + o] = 0.f;
+        if (lse != nullptr && lane < G) lse[(size_t)s * G + lane] = -INFINITY;
+      }
+      ++s;
+    }
+  };
+  QdPiece next = next_piece(__builtin_amdgcn_readfirstlane(
+      wave_upper_key(n_segments, from, lane, [&](int s) { return quant_first_scale(cap[s], s); })));
+  if (next.s < 0) return;
+  // Whether the whole block lies in this segment: the same in its four waves.
+  const int next_first = quant_first_scale(next.cap, next.s);
+  const bool together = next_first <= (int)blockIdx.x * kQdWaves * per_wave &&
+                        ((int)blockIdx.x + 1) * kQdWaves * per_wave <= next_first + (next.len + kQdTile - 1) / kQdTile;
+
+  // What a lane holds of a tile: bytes 64 w + 16 r .. + 15 of token 16 h + c of the keys, bytes 8 c .. 8 c + 7 of token
+  // 16 h + 4 r + e of the values.
+  uint4 kk[2][2];
+  uint2 vv[2][4];
+  float ks, vs;
+  auto load_keys = [&](int64_t row0, int last, int number) __attribute__((always_inline)) {   // rows past the end: the last row again
+    const uint8_t* base = rows.k + row0 * kHeadDim;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint8_t* p = kbase + (int64_t)min(t * kQdTile + 16 * h + c, last) * kHeadDim + 16 * r;   // past the end: the last row again
-      x.k[h][0] = load_stream16(reinterpret_cast<const uint4*>(p));
-      x.k[h][1] = load_stream16(reinterpret_cast<const uint4*>(p + 64));
+      const uint32_t at = (uint32_t)min(16 * h + c, last) * kHeadDim + 16 * r;
+      kk[h][0] = load_stream16(reinterpret_cast<const uint4*>(base + at));
+      kk[h][1] = load_stream16(reinterpret_cast<const uint4*>(base + at + 64));
     }
+    ks = rows.k_scale[number];
+    asm volatile("" ::: "memory");   // asked for here, not where they are used
+  };
+  auto load_values = [&](int64_t row0, int last, int number) __attribute__((always_inline)) {
+    const uint8_t* base = rows.v + row0 * kHeadDim;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const unsigned long long w = __builtin_nontemporal_load(reinterpret_cast<const unsigned long long*>(
-            vbase + (int64_t)min(t * kQdTile + 16 * h + 4 * r + e, last) * kHeadDim + 8 * c));
-        x.v[h][e] = make_uint2((uint32_t)w, (uint32_t)(w >> 32));
+        const uint32_t at = (uint32_t)min(16 * h + 4 * r + e, last) * kHeadDim + 8 * c;
+        const unsigned long long w = __builtin_nontemporal_load(reinterpret_cast<const unsigned long long*>(base + at));
+        vv[h][e] = make_uint2((uint32_t)w, (uint32_t)(w >> 32));
       }
-    x.ks = rows.k_scale[scale0 + t];
-    x.vs = rows.v_scale[scale0 + t];
+    vs = rows.v_scale[number];
+    asm volatile("" ::: "memory");
   };
-
   // B operand of the first product, columns past the group repeat its last head and are not used
   bf16x8_t qfrag[2][2];
-  {
-    const uint4* row = reinterpret_cast<const uint4*>(q + ((size_t)s * G + min(c, G - 1)) * kHeadDim);
+  auto load_q = [&](const QdPiece& x) __attribute__((always_inline)) {
+    const uint4* row = reinterpret_cast<const uint4*>(q + ((size_t)x.s * G + min(c, G - 1)) * kHeadDim);
 #pragma unroll
     for (int w = 0; w < 2; ++w)
 #pragma unroll
       for (int j = 0; j < 2; ++j) qfrag[w][j] = __builtin_bit_cast(bf16x8_t, row[8 * w + 2 * r + j]);
-  }
+  };
+  const float qscale = scale * kQdLog2e;
+
+  load_q(next);
+  // the tile that is asked for next: its first row, the last row of the segment from there, its scale number
+  int64_t row0 = (int64_t)next.cap + next.tile * kQdTile;
+  int last = next.len - next.tile * kQdTile - 1;
+  int number = next_first + next.tile;
+  load_keys(row0, last, number);
+  load_values(row0, last, number);
+#pragma unroll 1
+  for (;;) {
+  const QdPiece now = next;
   float m_run = -INFINITY, l_run = 0.f;   // running maximum of head c (log2 domain) in its four lanes, this lane's share of the denominator
+  float vs_run = 0.f;                     // largest value scale so far: the sums are in units of it
   f32x4_t acc[8];                         // O[head 4 r + e][channel 8 c + m]
 #pragma unroll
   for (int m = 0; m < 8; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const float qscale = scale * kQdLog2e;
+  next = next_piece(now.s + 1);   // while the rows are on their way
+  // waited for here: inside the loop the wait would reach the rows to come as well
+#pragma unroll
+  for (int w = 0; w < 2; ++w) asm volatile("" : "+v"(qfrag[w][0]), "+v"(qfrag[w][1]));
 
-  QdTile next;
-  if (wave < n_tiles) load_tile(next, wave);
+  // One set of registers a tile: the next tile's keys are asked for when this one's have been multiplied, its values likewise.
 #pragma unroll 1
-  for (int t = wave; t < n_tiles; t += kQdWaves) {
-    const QdTile x = next;
-    if (t + kQdWaves < n_tiles) load_tile(next, t + kQdWaves);
+  for (int t = now.tile; t < now.end; ++t) {
     f32x4_t sacc[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       sacc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<kFormat>(x.k[h][w].x, x.k[h][w].y), qfrag[w][0], sacc[h], 0, 0, 0);
-        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<kFormat>(x.k[h][w].z, x.k[h][w].w), qfrag[w][1], sacc[h], 0, 0, 0);
+        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(kk[h][w].x, kk[h][w].y), qfrag[w][0], sacc[h], 0, 0, 0);
+        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(kk[h][w].z, kk[h][w].w), qfrag[w][1], sacc[h], 0, 0, 0);
       }
     }
-    const float ts = qscale * x.ks;
+    const float ts = qscale * ks;
+    // Asked for in any case, so that the waits for this tile's values can count the loads behind them; behind a wave's last
+    // tile it is one row of it again.
+    if (t + 1 < now.end) {
+      row0 += kQdTile;
+      last -= kQdTile;
+      ++number;
+    } else if (next.s >= 0) {
+      row0 = (int64_t)next.cap + next.tile * kQdTile;
+      last = next.len - next.tile * kQdTile - 1;
+      number = quant_first_scale(next.cap, next.s) + next.tile;
+    } else {
+      last = 0;
+    }
+    load_keys(row0, last, number);
     float p[8];
     float mx = m_run;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < 8; ++i) p[i] = sacc[i >> 2][i & 3] * ts;
+    if ((t + 1) * kQdTile > now.len) {   // the segment's last tile
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        p[4 * h + e] = t * kQdTile + 16 * h + 4 * r + e < n_rows ? sacc[h][e] * ts : -INFINITY;
-        mx = fmaxf(mx, p[4 * h + e]);
-      }
+      for (int i = 0; i < 8; ++i)
+        if (t * kQdTile + 16 * (i >> 2) + 4 * r + (i & 3) >= now.len) p[i] = -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, p[i]);
     mx = max_over_row_blocks(mx);
-    const float alpha = qd_exp2(m_run - mx);   // 0 on the first tile
+    float alpha = qd_exp2(m_run - mx);   // 0 on the first tile
     m_run = mx;
     float psum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) { p[i] = qd_exp2(p[i] - mx); psum += p[i]; }
     l_run = l_run * alpha + psum;
-    bf16x8_t phigh, plow;   // the weights of the values' codes: rounded, and what the rounding left
+    const float vs_new = fmaxf(vs_run, vs);
+    const float unit = vs_new > 0.f ? 1.f / vs_new : 0.f;
+    const float ratio = vs * unit;
+    alpha *= vs_run * unit;
+    vs_run = vs_new;
+    f16x8_t phigh, plow;   // the weights of the values' codes, at most 1: rounded to f16, and what the rounding left
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float w = p[i] * x.vs;
-      phigh[i] = (__bf16)w;
-      plow[i] = (__bf16)(w - (float)phigh[i]);
+      const float w = p[i] * ratio;
+      phigh[i] = (_Float16)w;
+      plow[i] = (_Float16)(w - (float)phigh[i]);
     }
     if (__ballot(alpha != 1.f) != 0ull) {   // a maximum moved: the sums' rows are heads 4 r + e
       float al[4];
@@ -191,138 +268,223 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {   // channels 8 c + 4 b .. + 3
-      uint32_t v0[4], v1[4];
-      if (b == 0) {
-        transpose4(x.v[0][0].x, x.v[0][1].x, x.v[0][2].x, x.v[0][3].x, v0);
-        transpose4(x.v[1][0].x, x.v[1][1].x, x.v[1][2].x, x.v[1][3].x, v1);
-      } else {
-        transpose4(x.v[0][0].y, x.v[0][1].y, x.v[0][2].y, x.v[0][3].y, v0);
-        transpose4(x.v[1][0].y, x.v[1][1].y, x.v[1][2].y, x.v[1][3].y, v1);
+      // bytes of two tokens' four channels, side by side: [token pair][channels 4 b, 4 b + 1 or 4 b + 2, 4 b + 3]
+      uint32_t two[4][2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 first = vv[i >> 1][2 * (i & 1)], second = vv[i >> 1][2 * (i & 1) + 1];
+        uint32_t x = b == 0 ? first.x : first.y, y = b == 0 ? second.x : second.y;
+        two[i][0] = __builtin_amdgcn_perm(y, x, 0x05010400u);
+        two[i][1] = __builtin_amdgcn_perm(y, x, 0x07030602u);
+        if constexpr (kFormat == kQuantInt8) {
+          two[i][0] ^= 0x80808080u;
+          two[i][1] ^= 0x80808080u;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bf16x8_t vb = codes_to_bf16<kFormat>(v0[i], v1[i]);
-        acc[4 * b + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(phigh, vb, acc[4 * b + i], 0, 0, 0);
-        acc[4 * b + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(plow, vb, acc[4 * b + i], 0, 0, 0);
+        uint4 w;
+        if (i % 2 == 0)
+          w = make_uint4(two_values<kFormat, false>(two[0][i / 2]), two_values<kFormat, false>(two[1][i / 2]),
+                         two_values<kFormat, false>(two[2][i / 2]), two_values<kFormat, false>(two[3][i / 2]));
+        else
+          w = make_uint4(two_values<kFormat, true>(two[0][i / 2]), two_values<kFormat, true>(two[1][i / 2]),
+                         two_values<kFormat, true>(two[2][i / 2]), two_values<kFormat, true>(two[3][i / 2]));
+        const f16x8_t vb = __builtin_bit_cast(f16x8_t, w);
+        acc[4 * b + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(phigh, vb, acc[4 * b + i], 0, 0, 0);
+        acc[4 * b + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(plow, vb, acc[4 * b + i], 0, 0, 0);
       }
     }
+    load_values(row0, last, number);
   }
+#pragma unroll
+  for (int m = 0; m < 8; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[m][e] *= vs_run;
+  if (next.s >= 0) load_q(next);
   l_run = sum_over_row_blocks(l_run);
-
-  // the four waves' sums meet in LDS
-  const int per_wave = G * kHeadDim;
-  float* m_lds = merge_lds + kQdWaves * per_wave;
-  float* l_lds = m_lds + kQdWaves * G;
-  if (r == 0 && c < G) { m_lds[wave * G + c] = m_run; l_lds[wave * G + c] = l_run; }
+  if (together) {   // the only piece of each wave
+    const int per = G * kHeadDim;
+    float* m_lds = merge_lds + kQdWaves * per;
+    float* l_lds = m_lds + kQdWaves * G;
+    if (r == 0 && c < G) { m_lds[wave * G + c] = m_run; l_lds[wave * G + c] = l_run; }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int h = 4 * r + e;
+      if (h < G) {
+        float4* dst = reinterpret_cast<float4*>(merge_lds + wave * per + h * kHeadDim + 8 * c);
+        dst[0] = make_float4(acc[0][e], acc[1][e], acc[2][e], acc[3][e]);
+        dst[1] = make_float4(acc[4][e], acc[5][e], acc[6][e], acc[7][e]);
+      }
+    }
+    __syncthreads();
+    const size_t slot = (size_t)blockIdx.x * kQdWaves + now.s;
+    for (int o = tid; o < per; o += kQdThreads) {
+      const int h = o / kHeadDim;
+      float mx = m_lds[h];
+#pragma unroll
+      for (int w = 1; w < kQdWaves; ++w) mx = fmaxf(mx, m_lds[w * G + h]);
+      float num = 0.f, den = 0.f;
+#pragma unroll
+      for (int w = 0; w < kQdWaves; ++w) {
+        const float weight = qd_exp2(m_lds[w * G + h] - mx);
+        num = fmaf(merge_lds[w * per + o], weight, num);
+        den = fmaf(l_lds[w * G + h], weight, den);
+      }
+      ws_acc[slot * per + o] = num;
+      if (o % kHeadDim == 0) { ws_m[slot * G + h] = mx; ws_l[slot * G + h] = den; }
+    }
+    return;
+  }
+  const bool whole = now.tile == 0 && now.end * kQdTile >= now.len;
+  const size_t slot = (size_t)wave_id + now.s;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int h = 4 * r + e;
+    const float mxh = __shfl(m_run, h, 64), den = __shfl(l_run, h, 64);   // head h's are in lane h
     if (h < G) {
-      float4* dst = reinterpret_cast<float4*>(merge_lds + wave * per_wave + h * kHeadDim + 8 * c);
-      dst[0] = make_float4(acc[0][e], acc[1][e], acc[2][e], acc[3][e]);
-      dst[1] = make_float4(acc[4][e], acc[5][e], acc[6][e], acc[7][e]);
+      const float by = whole ? 1.f / den : 1.f;
+      float4* dst = reinterpret_cast<float4*>((whole ? out + ((size_t)now.s * G + h) * kHeadDim : ws_acc + (slot * G + h) * kHeadDim) + 8 * c);
+      dst[0] = make_float4(acc[0][e] * by, acc[1][e] * by, acc[2][e] * by, acc[3][e] * by);
+      dst[1] = make_float4(acc[4][e] * by, acc[5][e] * by, acc[6][e] * by, acc[7][e] * by);
+      if (c == 0) {
+        if (!whole) { ws_m[slot * G + h] = mxh; ws_l[slot * G + h] = den; }
+        else if (lse != nullptr) lse[(size_t)now.s * G + h] = mxh * kQdLn2 + __logf(den);
+      }
     }
   }
-  __syncthreads();
-  const bool whole = len <= chunk_rows;
-  for (int o = tid; o < per_wave; o += kQdThreads) {
-    const int h = o / kHeadDim;
-    float mx = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kQdWaves; ++w) mx = fmaxf(mx, m_lds[w * G + h]);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    float num = 0.f, den = 0.f;
-#pragma unroll
-    for (int w = 0; w < kQdWaves; ++w) {
-      const float weight = qd_exp2(m_lds[w * G + h] - ref);   // 0 for a wave without a tile
-      num = fmaf(merge_lds[w * per_wave + o], weight, num);
-      den = fmaf(l_lds[w * G + h], weight, den);
-    }
-    if (whole) {
-      out[(size_t)s * per_wave + o] = num / den;
-      if (o % kHeadDim == 0 && lse != nullptr) lse[(size_t)s * G + h] = mx * kQdLn2 + __logf(den);
-    } else {
-      ws_acc[(size_t)number * per_wave + o] = num;
-      if (o % kHeadDim == 0) { ws_m[(size_t)number * G + h] = mx; ws_l[(size_t)number * G + h] = den; }
-    }
+  if (next.s < 0) return;
   }
 }
 
-// The partials of a segment of several chunks: a block per segment and query head, a thread per channel, eight chunks' loads
-// in flight together.
-__global__ void __launch_bounds__(kQdMergeThreads)
-quant_decode_merge_kernel(const int32_t* __restrict__ cap, const int32_t* __restrict__ lengths, int chunk_rows, int G,
+// The pieces of a segment of several.  Half a wave holds the 128 channels of a segment's query head, four a lane, and has eight
+// pieces' loads in flight together.  kParts = 1: a block merges eight heads; else, where segments have many pieces, its eight half waves
+// share those of one head and their sums meet in LDS.
+constexpr int kQdHalf = 32;
+constexpr int kQdHalves = kQdThreads / kQdHalf;
+template <int kParts>
+__global__ void __launch_bounds__(kQdThreads)
+quant_decode_merge_kernel(const int32_t* __restrict__ cap, const int32_t* __restrict__ lengths, int n_heads, int per_wave, int G,
                           const float* __restrict__ ws_acc, const float* __restrict__ ws_m, const float* __restrict__ ws_l,
                           float* __restrict__ out, float* __restrict__ lse) {
-  const int s = blockIdx.x / G, h = blockIdx.x - s * G, ch = threadIdx.x;
+  const int half = threadIdx.x / kQdHalf, lane = threadIdx.x % kQdHalf;
+  const int row = kParts == 1 ? (int)blockIdx.x * kQdHalves + half : (int)blockIdx.x;
+  if (row >= n_heads) return;
+  const int s = row / G, h = row - s * G;
   const int lo = cap[s];
   const int len = lengths != nullptr ? lengths[s] : cap[s + 1] - lo;
-  if (len <= chunk_rows) return;   // finished, or empty
-  const int first = lo / chunk_rows + s, n = (int)(((int64_t)len + chunk_rows - 1) / chunk_rows);
+  const int first = quant_first_scale(lo, s), end = first + (int)(((int64_t)len + kQdTile - 1) / kQdTile);
+  const int w0 = first / per_wave, w1 = (end - 1) / per_wave;   // its waves
+  if (len <= 0 || w0 == w1) return;   // empty, or finished; with kParts > 1 the whole block
+  // blocks b0 .. b1 - 1 lie inside the segment and have a slot each, that of their first wave
+  const int per_block = per_wave * kQdWaves;
+  const int b0 = (first + per_block - 1) / per_block, b1 = max(end / per_block, b0);
+  const int ahead = b1 > b0 ? b0 * kQdWaves - w0 : w1 - w0 + 1;
+  const int n = b1 > b0 ? ahead + (b1 - b0) + (w1 + 1 - b1 * kQdWaves) : ahead;
   constexpr int kU = 8;
-  float mx = -INFINITY, num = 0.f, den = 0.f;
-  for (int i0 = 0; i0 < n; i0 += kU) {
-    float mv[kU], lv[kU], av[kU];
+  float mx = -INFINITY, den = 0.f;
+  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = kParts == 1 ? 0 : half * kU; i0 < n; i0 += kParts * kU) {
+    float mv[kU], lv[kU];
+    float4 av[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      const size_t at = (size_t)(first + min(i0 + u, n - 1)) * G + h;
+      const int i = min(i0 + u, n - 1);
+      const int w = i < ahead ? w0 + i : i < ahead + (b1 - b0) ? (b0 + i - ahead) * kQdWaves : b1 * kQdWaves + (i - ahead - (b1 - b0));
+      const size_t at = (size_t)(w + s) * G + h;
       mv[u] = ws_m[at];
       lv[u] = ws_l[at];
-      av[u] = ws_acc[at * kHeadDim + ch];
+      av[u] = reinterpret_cast<const float4*>(ws_acc + at * kHeadDim)[lane];
     }
     float top = mx;
 #pragma unroll
     for (int u = 0; u < kU; ++u) top = fmaxf(top, mv[u]);
     const float keep = qd_exp2(mx - top);
-    num *= keep;
+    num.x *= keep; num.y *= keep; num.z *= keep; num.w *= keep;
     den *= keep;
     mx = top;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
       const float weight = i0 + u < n ? qd_exp2(mv[u] - top) : 0.f;
-      num = fmaf(av[u], weight, num);
+      num.x = fmaf(av[u].x, weight, num.x);
+      num.y = fmaf(av[u].y, weight, num.y);
+      num.z = fmaf(av[u].z, weight, num.z);
+      num.w = fmaf(av[u].w, weight, num.w);
       den = fmaf(lv[u], weight, den);
     }
   }
-  const size_t row = (size_t)s * G + h;
-  out[row * kHeadDim + ch] = num / den;
-  if (ch == 0 && lse != nullptr) lse[row] = mx * kQdLn2 + __logf(den);
+  if constexpr (kParts > 1) {
+    __shared__ float4 num_lds[kQdHalves][kQdHalf];
+    __shared__ float mx_lds[kQdHalves], den_lds[kQdHalves];
+    num_lds[half][lane] = num;
+    if (lane == 0) { mx_lds[half] = mx; den_lds[half] = den; }
+    __syncthreads();
+    if (half > 0) return;
+#pragma unroll
+    for (int p = 1; p < kQdHalves; ++p) mx = fmaxf(mx, mx_lds[p]);
+    num = make_float4(0.f, 0.f, 0.f, 0.f);
+    den = 0.f;
+#pragma unroll
+    for (int p = 0; p < kQdHalves; ++p) {
+      const float weight = qd_exp2(mx_lds[p] - mx);   // 0 for a part without pieces
+      const float4 v = num_lds[p][lane];
+      num.x = fmaf(v.x, weight, num.x);
+      num.y = fmaf(v.y, weight, num.y);
+      num.z = fmaf(v.z, weight, num.z);
+      num.w = fmaf(v.w, weight, num.w);
+      den = fmaf(den_lds[p], weight, den);
+    }
+  }
+  const float by = 1.f / den;
+  reinterpret_cast<float4*>(out + (size_t)row * kHeadDim)[lane] = make_float4(num.x * by, num.y * by, num.z * by, num.w * by);
+  if (lane == 0 && lse != nullptr) lse[row] = mx * kQdLn2 + __logf(den);
 }
 
-// Rows of a chunk: a power of two.
-static int quant_decode_chunk_rows(int64_t total_rows) {
-  int c = kQdMinChunk;
-  while (c < (1 << 20) && total_rows / c > kQdTargetChunks) c *= 2;
-  return c;
+struct QdShape {
+  int numbers, per_wave, blocks;
+};
+
+static QdShape quant_decode_shape(int n_segments, int64_t total_rows) {
+  const int64_t numbers = total_rows / kQuantBlock + n_segments;
+  const int per_wave = (int)((numbers + kQdBlocks * kQdWaves - 1) / (kQdBlocks * kQdWaves));
+  const int64_t waves = (numbers + per_wave - 1) / per_wave;
+  return {(int)numbers, per_wave, (int)((waves + kQdWaves - 1) / kQdWaves)};
 }
 
-static int64_t quant_decode_chunks(int n_segments, int64_t total_rows) {
-  return total_rows / quant_decode_chunk_rows(total_rows) + n_segments;
+static size_t quant_decode_slots(int n_segments, int64_t total_rows) {
+  return (size_t)quant_decode_shape(n_segments, total_rows).blocks * kQdWaves + n_segments;
 }
 
 size_t quant_decode_workspace_bytes(int n_segments, int64_t total_rows, int G) {
-  const size_t bytes = (size_t)quant_decode_chunks(n_segments, total_rows) * G * (kHeadDim + 2) * sizeof(float);
+  if (n_segments < 1) return 0;
+  const size_t bytes = quant_decode_slots(n_segments, total_rows) * G * (kHeadDim + 2) * sizeof(float);
   return (bytes + 255) & ~(size_t)255;
 }
 
 hipError_t launch_quant_decode(int format, int G, const void* q, const QuantRows& rows, const int32_t* cap, const int32_t* lengths,
                                int n_segments, int64_t total_rows, float scale, float* out, float* lse, float* ws, hipStream_t stream) {
   if (G < 1 || G > kDecodeMaxGroup) return hipErrorInvalidValue;
-  const int chunk_rows = quant_decode_chunk_rows(total_rows);
-  const int64_t chunks = quant_decode_chunks(n_segments, total_rows);
+  const QdShape shape = quant_decode_shape(n_segments, total_rows);
+  const size_t slots = quant_decode_slots(n_segments, total_rows);
   float* ws_acc = ws;
-  float* ws_m = ws + (size_t)chunks * G * kHeadDim;
-  float* ws_l = ws_m + (size_t)chunks * G;
+  float* ws_m = ws + slots * G * kHeadDim;
+  float* ws_l = ws_m + slots * G;
   const size_t lds = (size_t)kQdWaves * G * (kHeadDim + 2) * sizeof(float);   // at most 33 KB
   auto launch = [&](auto tag) {
-    hipLaunchKernelGGL((quant_decode_kernel<decltype(tag)::value>), dim3((unsigned)chunks), dim3(kQdThreads), lds, stream,
-                       static_cast<const uint16_t*>(q), rows, cap, lengths, n_segments, chunk_rows, G, scale, out, lse, ws_acc, ws_m, ws_l);
+    hipLaunchKernelGGL((quant_decode_kernel<decltype(tag)::value>), dim3(shape.blocks), dim3(kQdThreads), lds, stream,
+                       static_cast<const uint16_t*>(q), rows, cap, lengths, n_segments, shape.numbers, shape.per_wave, G, scale, out, lse,
+                       ws_acc, ws_m, ws_l);
   };
   if (format == kQuantE4m3) launch(std::integral_constant<int, kQuantE4m3>{});
   else launch(std::integral_constant<int, kQuantInt8>{});
-  if (total_rows > chunk_rows)   // else no segment has two chunks
-    hipLaunchKernelGGL(quant_decode_merge_kernel, dim3((unsigned)((int64_t)n_segments * G)), dim3(kQdMergeThreads), 0, stream, cap, lengths,
-                       chunk_rows, G, ws_acc, ws_m, ws_l, out, lse);
+  auto merge = [&](auto tag) {
+    constexpr int kParts = decltype(tag)::value;
+    const int n_heads = n_segments * G;
+    hipLaunchKernelGGL((quant_decode_merge_kernel<kParts>), dim3(kParts == 1 ? (n_heads + kQdHalves - 1) / kQdHalves : n_heads),
+                       dim3(kQdThreads), 0, stream, cap, lengths, n_heads, shape.per_wave, G, ws_acc, ws_m, ws_l, out, lse);
+  };
+  if (shape.blocks > kQdManyPieces * n_segments) merge(std::integral_constant<int, kQdHalves>{});
+  else merge(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
 
