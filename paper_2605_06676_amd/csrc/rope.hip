@@ -3,11 +3,15 @@
 // the other channels are copied.  The backward pass is the transpose, the same turn by the negative angle (the sine's sign).
 //
 // The call moves every element once in and once out and is bound by that; what could get in the way are the cosines and sines.
-// They are fp64 work (lkv_rotary.h), the same for all heads of a token, so a block takes 8 tokens and many heads: its 256
-// threads compute the 8 x 64 cosines and sines of the tokens once, into LDS, and each wave then turns head after head, with the
-// 16 of its lanes in registers.  A lane has 8 pairs: 16 channels, which in bf16 are two 16-byte pieces, and 8 lanes make a row.
-// Calls too short to fill the chip so are cut along the heads as well.
-#include <algorithm>
+// They are fp64 work (lkv_rotary.h), the same for all heads of a token, so a block takes 32 tokens of a few heads and its 256
+// threads compute the tokens' cosines and sines once, into LDS.  The rows of a head are contiguous in the usual layouts, so the heads of a block are
+// few: a wave has 32 rows of one.  A lane has two 16-byte pieces of a row, such that the same piece of neighbouring lanes is contiguous (128
+// bytes of a row at least).  A wave asks for its first rows before the cosines.
+//
+// Blocks follow memory: those that run together lie together, whichever of heads and tokens is the inner one.  With the heads inside
+// where the tokens are, strides of a power of two put the rows in flight on few channels: 32 heads of 16384 tokens in bf16 59.4 us, 53.9 (5.0
+// TB/s) so; 32 of 8192 in fp32 73.6 and 51.2; but 32 batches of 32 heads of 512 tokens 50.0 and 63.3, which the batches outside mend.
+// Few heads leave the cosines as the bound: one head of 524288 tokens 105 us.
 #include <type_traits>
 
 #include "lkv_kernels.h"
@@ -16,37 +20,27 @@ namespace lkv {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWaves = kRopeThreads / 64;
-constexpr int kRopeTokens = 8;
+constexpr int kRopeTokens = 32;     // of a block
 constexpr int kRopePairs = kHeadDim / 2;
-constexpr int kRopeUnroll = 4;     // heads of a wave whose loads are in flight together
-constexpr int kRopeBlocks = 1024;   // blocks that a launch wants: 4 per compute unit
+constexpr int kRopeUnroll = 4;      // loads of a wave in flight together: as many times 64 lanes of pieces
+constexpr int kRopeHeads = 4;       // of a block
 
-template <typename T> struct RopePiece;   // 8 elements
-template <> struct RopePiece<uint16_t> {
-  uint4 w;
-  __device__ __forceinline__ void load(const uint16_t* p) { w = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void get(float (&f)[8]) const { unpack8(w, f); }
-  static __device__ __forceinline__ uint32_t two(float a, float b) {
-    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
-    const bf16x2 v = {(__bf16)a, (__bf16)b};
-    return __builtin_bit_cast(uint32_t, v);
-  }
-  __device__ __forceinline__ void set(const float (&f)[8]) { w = make_uint4(two(f[0], f[1]), two(f[2], f[3]), two(f[4], f[5]), two(f[6], f[7])); }
-  __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<uint4*>(p) = w; }
-};
-template <> struct RopePiece<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-  }
-  __device__ __forceinline__ void set(const float (&f)[8]) {
-    a = make_float4(f[0], f[1], f[2], f[3]);
-    b = make_float4(f[4], f[5], f[6], f[7]);
-  }
-  __device__ __forceinline__ void store(float* p) const { reinterpret_cast<float4*>(p)[0] = a; reinterpret_cast<float4*>(p)[1] = b; }
-};
-
+// Elements of a 16-byte piece as fp32, and back.
+__device__ __forceinline__ void rope_unpack(const uint4& w, float (&f)[8]) { unpack8(w, f); }
+__device__ __forceinline__ void rope_unpack(const uint4& w, float (&f)[4]) {
+  f[0] = __uint_as_float(w.x); f[1] = __uint_as_float(w.y); f[2] = __uint_as_float(w.z); f[3] = __uint_as_float(w.w);
+}
+__device__ __forceinline__ uint32_t rope_two(float a, float b) {
+  typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ uint4 rope_pack(const float (&f)[8]) {
+  return make_uint4(rope_two(f[0], f[1]), rope_two(f[2], f[3]), rope_two(f[4], f[5]), rope_two(f[6], f[7]));
+}
+__device__ __forceinline__ uint4 rope_pack(const float (&f)[4]) {
+  return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
 __device__ __forceinline__ float rope_get(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ float rope_get(float x) { return x; }
 template <typename T> __device__ __forceinline__ T rope_put(float f) {
@@ -54,103 +48,130 @@ template <typename T> __device__ __forceinline__ T rope_put(float f) {
   else return f;
 }
 
-// kWide: rotary_dim is a multiple of 16, so that the 8 pairs of a lane are whole pieces.  Else a lane takes one pair at a time.
+// kWide: the rotated channels of either half are whole pieces (rotary_dim a multiple of 16 in bf16 and of 8 in fp32).  Else
+// a lane takes one pair at a time.
 template <typename T, bool kWide>
 __global__ void __launch_bounds__(kRopeThreads)
 rope_kernel(RotaryArgs rot, const T* x, RopeStrides xs, T* y, RopeStrides ys, const int32_t* __restrict__ positions,
-            int64_t positions_stride, int first_position, int n_tokens, int64_t n_rows /* batch x tokens */, int n_heads,
-            int heads_per_block, int head_blocks, float sign) {
+            int64_t positions_stride, int first_position, uint32_t n_tokens, uint32_t run /* rows that a block may join */, int n_heads,
+            uint32_t head_blocks, bool heads_inside, float sign) {
   __shared__ __align__(16) float cos_lds[kRopeTokens][kRopePairs];
   __shared__ __align__(16) float sin_lds[kRopeTokens][kRopePairs];
   const int tid = threadIdx.x;
-  const int64_t row0 = (int64_t)(blockIdx.x / (unsigned)head_blocks) * kRopeTokens;
-  const int h0 = (int)(blockIdx.x % (unsigned)head_blocks) * heads_per_block;
-  const int h1 = min(h0 + heads_per_block, n_heads);
+  // rows are (batch, token) pairs
+  const uint32_t run_blocks = (run + kRopeTokens - 1) / kRopeTokens, which = blockIdx.x / (head_blocks * run_blocks);
+  const uint32_t inner = blockIdx.x - which * head_blocks * run_blocks;
+  const uint32_t hb = heads_inside ? inner % head_blocks : inner / run_blocks, rb = heads_inside ? inner / head_blocks : inner % run_blocks;
+  const uint32_t row0 = which * run + rb * kRopeTokens;
+  const int h0 = (int)hb * kRopeHeads;
+  const int heads = min(kRopeHeads, n_heads - h0), tokens = (int)min((uint32_t)kRopeTokens, run - rb * kRopeTokens);
   const int half = rot.rotary_dim >> 1;
 
-  for (int i = tid; i < kRopeTokens * kRopePairs; i += kRopeThreads) {
-    const int pair = i % kRopePairs;
-    const int64_t row = row0 + i / kRopePairs;
-    float c = 1.f, s = 0.f;
-    if (pair < half && row < n_rows) {
-      const int64_t b = row / n_tokens;
-      const int t = (int)(row - b * n_tokens);
-      const int pos = positions != nullptr ? positions[b * positions_stride + t] : first_position + t;
-      rotary_cos_sin(pos, rot.inv_freq[pair], rot.factor, &c, &s);
+  auto fill_tables = [&]() __attribute__((always_inline)) {
+    const int pair = tid % kRopePairs;   // the same in every turn
+    const double w = rot.inv_freq[min(pair, half - 1)];
+    for (int token = tid / kRopePairs; token < tokens; token += kRopeThreads / kRopePairs) {
+      const uint32_t b = (row0 + token) / n_tokens, t = row0 + token - b * n_tokens;
+      float c, s;
+      rotary_cos_sin(positions != nullptr ? positions[b * positions_stride + t] : first_position + (int)t, w, rot.factor, &c, &s);
+      cos_lds[token][pair] = c;
+      sin_lds[token][pair] = s * sign;
     }
-    cos_lds[i / kRopePairs][pair] = c;
-    sin_lds[i / kRopePairs][pair] = s * sign;
-  }
-  __syncthreads();
+    __syncthreads();
+  };
 
   const int wave = tid >> 6, lane = tid & 63;
   if constexpr (kWide) {
-    const int token = lane >> 3, octet = lane & 7;
-    const int64_t row = row0 + token;
-    if (row >= n_rows) return;
-    const int64_t b = row / n_tokens;
-    const int64_t t = row - b * n_tokens;
-    const bool turned = octet * 8 < half;
-    // this lane's two pieces of 8 channels
-    const bool split = turned && rot.pairs == 0;
-    const int ch0 = split ? octet * 8 : octet * 16;
-    const int ch1 = split ? octet * 8 + half : octet * 16 + 8;
-    float c[8], s[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { c[i] = cos_lds[token][octet * 8 + i]; s[i] = sin_lds[token][octet * 8 + i]; }
-    const T* px = x + b * xs.batch + t * xs.token;
-    T* py = y + b * ys.batch + t * ys.token;
-    // y may be x: the loads of a round go ahead of its stores by hand
-    for (int h = h0 + wave; h < h1; h += kRopeWaves * kRopeUnroll) {
-      RopePiece<T> p0[kRopeUnroll], p1[kRopeUnroll];
+    constexpr int kPiece = 16 / (int)sizeof(T);              // elements
+    constexpr int kLanes = kHeadDim / (2 * kPiece);          // of a row
+    constexpr int kRows = 64 / kLanes;                       // of a wave's load
+    // the block's loads, head after head, dealt to the waves in equal runs
+    const int groups = (tokens + kRows - 1) / kRows;
+    const int each = (heads * groups + kRopeWaves - 1) / kRopeWaves;
+    const int item0 = wave * each, item1 = min(item0 + each, heads * groups);
+    const int at = lane % kLanes;
+    // this lane's two pieces, and whether they are turned: with each other (halves) or in themselves (pairs)
+    const bool halves = rot.pairs == 0;
+    const int turned_lanes = half / kPiece;                  // halves: lanes of rotated channels; the others share the rest likewise
+    const bool turned0 = halves ? at < turned_lanes : at * kPiece < rot.rotary_dim;
+    const bool turned1 = halves ? turned0 : kRopePairs + at * kPiece < rot.rotary_dim;
+    const int rest = rot.rotary_dim + (at - turned_lanes) * kPiece;
+    const int ch0 = !halves ? at * kPiece : turned0 ? at * kPiece : rest;
+    const int ch1 = !halves ? kRopePairs + at * kPiece : turned0 ? half + at * kPiece : rest + (kHeadDim - rot.rotary_dim) / 2;
+    uint4 p0[kRopeUnroll], p1[kRopeUnroll];
+    int64_t out[kRopeUnroll];   // where a row goes, -1: nowhere
+    int token[kRopeUnroll];
+    auto load = [&](int item) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < kRopeUnroll; ++u) {
-        const T* p = px + min(h + u * kRopeWaves, h1 - 1) * xs.head;   // past the last head: read, not written
-        p0[u].load(p + ch0);
-        p1[u].load(p + ch1);
+        const int i = min(item + u, heads * groups - 1);     // past the last: read, not written
+        const int h = i / groups;
+        token[u] = (i - h * groups) * kRows + lane / kLanes;
+        const bool live = item + u < item1 && token[u] < tokens;
+        token[u] = min(token[u], tokens - 1);
+        const uint32_t row = row0 + token[u], b = row / n_tokens, t = row - b * n_tokens;
+        const T* p = x + (int64_t)b * xs.batch + (int64_t)(h0 + h) * xs.head + (int64_t)t * xs.token;
+        p0[u] = *reinterpret_cast<const uint4*>(p + ch0);
+        p1[u] = *reinterpret_cast<const uint4*>(p + ch1);
+        out[u] = live ? (int64_t)b * ys.batch + (int64_t)(h0 + h) * ys.head + (int64_t)t * ys.token : -1;
       }
+    };
+    load(item0);
+    fill_tables();
+    // y may be x: nothing is read after it has been written
+    for (int item = item0; item < item1; item += kRopeUnroll) {
+      if (item > item0) load(item);
 #pragma unroll
       for (int u = 0; u < kRopeUnroll; ++u) {
-        if (h + u * kRopeWaves >= h1) break;
-        if (turned) {
-          float f0[8], f1[8];
-          p0[u].get(f0);
-          p1[u].get(f1);
-          if (rot.pairs == 0) {
+        float f0[kPiece], f1[kPiece];
+        rope_unpack(p0[u], f0);
+        rope_unpack(p1[u], f1);
+        const float* c = cos_lds[token[u]];
+        const float* s = sin_lds[token[u]];
+        if (halves) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) rotary_turn(f0[i], f1[i], c[i], s[i]);
-          } else {
+          for (int i = 0; i < kPiece; ++i) rotary_turn(f0[i], f1[i], c[at * kPiece + i], s[at * kPiece + i]);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              rotary_turn(f0[2 * i], f0[2 * i + 1], c[i], s[i]);
-              rotary_turn(f1[2 * i], f1[2 * i + 1], c[4 + i], s[4 + i]);
-            }
+          for (int i = 0; i < kPiece / 2; ++i) {
+            const int pair = at * (kPiece / 2) + i;
+            rotary_turn(f0[2 * i], f0[2 * i + 1], c[pair], s[pair]);
+            rotary_turn(f1[2 * i], f1[2 * i + 1], c[kRopePairs / 2 + pair], s[kRopePairs / 2 + pair]);
           }
-          p0[u].set(f0);
-          p1[u].set(f1);
         }
-        T* p = py + (h + u * kRopeWaves) * ys.head;
-        p0[u].store(p + ch0);
-        p1[u].store(p + ch1);
+        if (out[u] >= 0) {   // a piece that is not turned goes bit for bit
+          store_stream16(reinterpret_cast<uint4*>(y + out[u] + ch0), turned0 ? rope_pack(f0) : p0[u]);
+          store_stream16(reinterpret_cast<uint4*>(y + out[u] + ch1), turned1 ? rope_pack(f1) : p1[u]);
+        }
       }
     }
   } else {
+    fill_tables();
     const int ch0 = lane < half && rot.pairs == 0 ? lane : 2 * lane;
     const int ch1 = lane < half && rot.pairs == 0 ? lane + half : 2 * lane + 1;
-    for (int token = 0; token < kRopeTokens; ++token) {
-      const int64_t row = row0 + token;
-      if (row >= n_rows) return;
-      const int64_t b = row / n_tokens;
-      const int64_t t = row - b * n_tokens;
-      const float c = cos_lds[token][lane], s = sin_lds[token][lane];
-      const T* px = x + b * xs.batch + t * xs.token;
-      T* py = y + b * ys.batch + t * ys.token;
-      for (int h = h0 + wave; h < h1; h += kRopeWaves) {
-        const T x0 = px[h * xs.head + ch0], x1 = px[h * xs.head + ch1];
-        float a0 = rope_get(x0), a1 = rope_get(x1);
-        rotary_turn(a0, a1, c, s);
-        py[h * ys.head + ch0] = lane < half ? rope_put<T>(a0) : x0;
-        py[h * ys.head + ch1] = lane < half ? rope_put<T>(a1) : x1;
+    // y may be x: a round's loads go ahead of its stores by hand
+    for (int i0 = wave; i0 < heads * tokens; i0 += kRopeWaves * kRopeUnroll) {
+      T x0[kRopeUnroll], x1[kRopeUnroll];
+      int64_t out[kRopeUnroll];
+      int token[kRopeUnroll];
+#pragma unroll
+      for (int u = 0; u < kRopeUnroll; ++u) {
+        const int i = min(i0 + u * kRopeWaves, heads * tokens - 1);   // past the last: read, not written
+        const int h = i / tokens;
+        token[u] = i - h * tokens;
+        const uint32_t row = row0 + token[u], b = row / n_tokens, t = row - b * n_tokens;
+        const T* p = x + (int64_t)b * xs.batch + (int64_t)(h0 + h) * xs.head + (int64_t)t * xs.token;
+        x0[u] = p[ch0];
+        x1[u] = p[ch1];
+        out[u] = (int64_t)b * ys.batch + (int64_t)(h0 + h) * ys.head + (int64_t)t * ys.token;
+      }
+#pragma unroll
+      for (int u = 0; u < kRopeUnroll; ++u) {
+        if (i0 + u * kRopeWaves >= heads * tokens) break;
+        float a0 = rope_get(x0[u]), a1 = rope_get(x1[u]);
+        rotary_turn(a0, a1, cos_lds[token[u]][lane], sin_lds[token[u]][lane]);
+        y[out[u] + ch0] = lane < half ? rope_put<T>(a0) : x0[u];   // not turned: bit for bit
+        y[out[u] + ch1] = lane < half ? rope_put<T>(a1) : x1[u];
       }
     }
   }
@@ -159,18 +180,18 @@ rope_kernel(RotaryArgs rot, const T* x, RopeStrides xs, T* y, RopeStrides ys, co
 void launch_rope(const RotaryArgs& rot, bool f32, const void* x, const RopeStrides& xs, void* y, const RopeStrides& ys,
                  const int32_t* positions, int64_t positions_stride, int first_position, int n_batch, int n_heads, int n_tokens,
                  bool backward, hipStream_t stream) {
-  const int64_t n_rows = (int64_t)n_batch * n_tokens;
-  const int64_t token_blocks = (n_rows + kRopeTokens - 1) / kRopeTokens;
-  int head_blocks = (int)std::min<int64_t>((n_heads + kRopeWaves - 1) / kRopeWaves, std::max<int64_t>(1, kRopeBlocks / token_blocks));
-  const int per_block = ((n_heads + head_blocks - 1) / head_blocks + kRopeWaves - 1) / kRopeWaves * kRopeWaves;
-  head_blocks = (n_heads + per_block - 1) / per_block;
+  const uint32_t n_rows = (uint32_t)((int64_t)n_batch * n_tokens);
+  const uint32_t run = n_tokens >= kRopeTokens ? (uint32_t)n_tokens : n_rows;   // short ones are joined across batches
+  const uint32_t blocks = n_rows / run * ((run + kRopeTokens - 1) / kRopeTokens);
+  const uint32_t head_blocks = (uint32_t)(n_heads + kRopeHeads - 1) / kRopeHeads;
+  const bool heads_inside = xs.head < xs.token;
   auto launch = [&](auto tag, auto wide) {
     using T = decltype(tag);
-    hipLaunchKernelGGL((rope_kernel<T, decltype(wide)::value>), dim3((unsigned)(token_blocks * head_blocks)), dim3(kRopeThreads), 0,
-                       stream, rot, static_cast<const T*>(x), xs, static_cast<T*>(y), ys, positions, positions_stride, first_position,
-                       n_tokens, n_rows, n_heads, per_block, head_blocks, backward ? -1.f : 1.f);
+    hipLaunchKernelGGL((rope_kernel<T, decltype(wide)::value>), dim3(blocks * head_blocks), dim3(kRopeThreads), 0, stream, rot,
+                       static_cast<const T*>(x), xs, static_cast<T*>(y), ys, positions, positions_stride, first_position,
+                       (uint32_t)n_tokens, run, n_heads, head_blocks, heads_inside, backward ? -1.f : 1.f);
   };
-  const bool wide = rot.rotary_dim % 16 == 0;
+  const bool wide = rot.rotary_dim % (f32 ? 8 : 16) == 0;
   if (f32) { if (wide) launch(float{}, std::true_type{}); else launch(float{}, std::false_type{}); }
   else { if (wide) launch(uint16_t{}, std::true_type{}); else launch(uint16_t{}, std::false_type{}); }
 }

@@ -72,6 +72,8 @@ class _RopeScaling(C.Structure):
                 ("trained_len", C.c_double), ("low", C.c_double), ("high", C.c_double)]
 
 
+_Strides = C.c_int64 * 3
+
 _lib = None
 
 
@@ -706,15 +708,14 @@ def lkv_rope(ctx: Context, rotary: Rotary, x, y, positions=None, first_position:
     assert x.shape == y.shape and x.dtype == y.dtype and x.dtype in (torch.bfloat16, torch.float32) and x.dim() in (3, 4)
     assert x.is_cuda and y.is_cuda and x.stride(-1) == 1 and y.stride(-1) == 1
     B, Hn, T, d = x.shape if x.dim() == 4 else (1, *x.shape)
-
-    def strides(t):   # of a single batch, head or token: never followed
-        s = t.stride()[:-1] if t.dim() == 4 else (0, *t.stride()[:-1])
-        return (C.c_int64 * 3)(*[0 if n == 1 else st for n, st in zip((B, Hn, T), s)])
-
+    # the stride of a single batch, head or token is never followed
+    sx, sy = x.stride(), y.stride()
+    xs = _Strides(sx[0] if B > 1 else 0, sx[-3] if Hn > 1 else 0, sx[-2] if T > 1 else 0)
+    ys = _Strides(sy[0] if B > 1 else 0, sy[-3] if Hn > 1 else 0, sy[-2] if T > 1 else 0)
     step = 0
     if positions is not None:
         assert positions.dtype == torch.int32 and positions.is_cuda and positions.shape[-1] == T and (T == 1 or positions.stride(-1) == 1)
         assert positions.dim() == 1 or positions.shape == (B, T)
         step = positions.stride(0) if positions.dim() == 2 and B > 1 else 0
-    ctx._check(ctx.lib.lkv_rope(ctx.h, C.byref(rotary.c), 1 if x.dtype == torch.float32 else 0, B, Hn, T, d, _ptr(x), strides(x),
-                                _ptr(y), strides(y), _ptr(positions), step, int(first_position), int(backward), _stream_ptr(stream)))
+    ctx._check(ctx.lib.lkv_rope(ctx.h, C.byref(rotary.c), 1 if x.dtype == torch.float32 else 0, B, Hn, T, d, _ptr(x), xs,
+                                _ptr(y), ys, _ptr(positions), step, int(first_position), int(backward), _stream_ptr(stream)))
