@@ -467,7 +467,8 @@ lkv_status lkv_rope_frequencies(const lkv_rope_scaling *scaling, double *inv_fre
  * dtype      : of x and y: LKV_BF16 (q, k) or LKV_FP32 (their gradients as lkv_masked_attn_backward writes them); the
  *              rotation is fp32 with cosine and sine good to fp32 at any position
  * x, y       : DEVICE; y may be x (then with the same strides), and must not overlap it otherwise
- * x_strides, y_strides : HOST int64 [3], elements between batches, heads and tokens; multiples of 16 bytes
+ * x_strides, y_strides : HOST int64 [3], elements between batches, heads and tokens; multiples of 16 bytes; those of x may be
+ *              0 (a broadcast input), those of y only where there is one batch, head or token
  * positions  : DEVICE int32, position of token t of batch b at [b * positions_stride + t] (stride 0: one row for all);
  *              or NULL: first_position + t
  * backward   : 0, or 1: the transposed map, which takes the gradient of y to that of x */

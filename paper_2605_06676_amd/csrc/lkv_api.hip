@@ -1046,6 +1046,9 @@ lkv_status lkv_rope(lkv_ctx* ctx, const lkv_rotary* rotary, int32_t dtype, int32
   for (int i = 0; i < 3; ++i)
     if (x_strides[i] % piece != 0 || y_strides[i] % piece != 0)
       return fail(ctx, LKV_ERR_INVALID_ARG, "stride %d of x or y is not a multiple of 16 bytes", i);
+  const int32_t sizes[3] = {n_batch, n_heads, n_tokens};
+  for (int i = 0; i < 3; ++i)
+    if (sizes[i] > 1 && y_strides[i] == 0) return fail(ctx, LKV_ERR_INVALID_ARG, "stride %d of y is 0: rows would be written over each other", i);
   if (backward != 0 && backward != 1) return fail(ctx, LKV_ERR_INVALID_ARG, "backward must be 0 or 1");
   if (positions == nullptr && (int64_t)first_position + n_tokens > (int64_t)1 << 31)
     return fail(ctx, LKV_ERR_INVALID_ARG, "first_position + n_tokens exceeds 2^31");

@@ -84,6 +84,12 @@ __device__ __forceinline__ uint32_t two_values(uint32_t w) {
   }
 }
 
+// Rows of a segment: never more than it owns, whatever `lengths` says.
+__device__ __forceinline__ int rows_in_use(const int32_t* __restrict__ cap, const int32_t* __restrict__ lengths, int s) {
+  const int room = cap[s + 1] - cap[s];
+  return max(lengths != nullptr ? min(lengths[s], room) : room, 0);
+}
+
 // The part of a segment that a wave has.
 struct QdPiece {
   int s;               // -1: none
@@ -111,7 +117,7 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
     QdPiece x;
     x.s = s;
     x.cap = __builtin_amdgcn_readfirstlane(cap[s]);   // the same in all lanes: kept in scalar registers
-    x.len = __builtin_amdgcn_readfirstlane(max(lengths != nullptr ? lengths[s] : cap[s + 1] - x.cap, 0));
+    x.len = __builtin_amdgcn_readfirstlane(rows_in_use(cap, lengths, s));
     const int first = quant_first_scale(x.cap, s);
     x.tile = max(from - first, 0);
     x.end = min(to - first, (x.len + kQdTile - 1) / kQdTile);
@@ -372,7 +378,7 @@ quant_decode_merge_kernel(const int32_t* __restrict__ cap, const int32_t* __rest
   if (row >= n_heads) return;
   const int s = row / G, h = row - s * G;
   const int lo = cap[s];
-  const int len = lengths != nullptr ? lengths[s] : cap[s + 1] - lo;
+  const int len = rows_in_use(cap, lengths, s);
   const int first = quant_first_scale(lo, s), end = first + (int)(((int64_t)len + kQdTile - 1) / kQdTile);
   const int w0 = first / per_wave, w1 = (end - 1) / per_wave;   // its waves
   if (len <= 0 || w0 == w1) return;   // empty, or finished; with kParts > 1 the whole block

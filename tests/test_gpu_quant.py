@@ -288,6 +288,66 @@ def test_decode_reads_nothing_of_spare_rows(ctx, fmt):
     assert np.array_equal(out, again[0]) and np.array_equal(lse, again[1])
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_rows_past_two_to_the_31_bytes(ctx, fmt):
+    """Two segments, the second 17 million rows further on: decode, append and re-eviction reach it; and a compaction from a head
+    of 9 million tokens."""
+    gap = 17_000_000
+    cap, lengths = np.array([0, gap, gap + 200]), np.array([70, 90])
+    n = Q.scale_count(2, int(cap[-1]))
+    codes = [torch.zeros((int(cap[-1]), 128), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros(n, device="cuda") for _ in range(2)]
+    rows = lkv.QuantRows(codes[0].view(KINDS[fmt]), codes[1].view(KINDS[fmt]), *scales)
+    small, small_cap = _filled(lengths, 110, fmt, 17)                    # the same values in a small cache
+    for s, m in enumerate(lengths):
+        for big, bs, sc, ss in ((codes[0], scales[0], small.kc, small.ks), (codes[1], scales[1], small.vc, small.vs)):
+            big[cap[s]:cap[s] + m] = torch.from_numpy(sc[small_cap[s]:small_cap[s] + m]).cuda()
+            for b in range(0, m, 32):
+                bs[Q.scale_number(cap[s], s, b)] = float(ss[Q.scale_number(small_cap[s], s, b)])
+    q = _queries(1, 1, 8, 18).cuda()
+    d_cap, d_len, total = i32(cap), i32(lengths), int(cap[-1])
+    out, lse = torch.full((8, 128), float("nan"), device="cuda"), torch.full((8,), float("nan"), device="cuda")
+    ws = torch.empty(lkv.lkv_decode_quant_workspace_bytes(2, total, 8, 2), dtype=torch.uint8, device="cuda")
+    lkv.lkv_decode_attn_quant(ctx, 1, 1, 2, 8, 128, q, rows, d_cap, d_len, total, 0.09, out, lse, ws)
+    _assert_decode(small, small_cap, lengths, q.cpu(), 2, 0.09, out.cpu().numpy(), lse.cpu().numpy())
+    new = torch.randn((2, 1, 1, 2, 128), generator=torch.Generator().manual_seed(19)).to(torch.bfloat16).cuda()
+    small_len = i32(lengths)
+    lkv.lkv_append_quant(ctx, 1, 1, 2, 128, new[0], new[1], rows, d_cap, d_len)
+    lkv.lkv_append_quant(ctx, 1, 1, 2, 128, new[0], new[1], small.c, i32(small_cap), small_len)
+    assert torch.equal(d_len, small_len)
+    up = torch.zeros(total, device="cuda")
+    up[cap[1]:cap[1] + 91] = torch.randn(91, generator=torch.Generator().manual_seed(20)).cuda()
+    small_up = torch.zeros(small.rows, device="cuda")
+    small_up[small_cap[1]:small_cap[1] + 91] = up[cap[1]:cap[1] + 91]
+    got = []
+    for src, u, c, ln in ((rows, up, d_cap, d_len), (small.c, small_up, i32(small_cap), small_len)):
+        p = Packed(60, 2, fmt)
+        u2, c2, l2, idx, off = torch.zeros(60, device="cuda"), i32([0, 0, 0]), i32([0, 0]), i32(np.zeros(60)), i32([0, 0, 0])
+        lkv.lkv_reevict_quant(ctx, 128, src, u, c, ln, [71, 91], [15, 41], 2, idx, off, p.c, u2, c2, l2)
+        got.append([x.clone() for x in p.dev] + [u2, c2, l2])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    del rows, codes, scales, up, got
+    torch.cuda.empty_cache()
+    T = 9_000_000
+    k = torch.zeros((1, 1, T, 128), dtype=torch.bfloat16, device="cuda")
+    pick = torch.tensor([0, 5, T - 70, T - 3, T - 1])
+    k[0, 0, pick] = torch.randn((5, 128), generator=torch.Generator().manual_seed(21)).to(torch.bfloat16).cuda()
+    p = Packed(5, 1, fmt)
+    Q.write_segment(k[0, 0, pick].double().cpu().numpy(), 0, 0, p.kc, p.ks, fmt)
+    p.vc[:5], p.vs[0] = p.kc[:5], p.ks[0]
+    lkv.lkv_compact_quant(ctx, lkv.Cache([k], [k], 1), pick.int().cuda(), i32([0, 5]), 5, p.c)
+    p.assert_same("compact")
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_lengths_beyond_their_segment_are_cut(ctx, fmt):
+    lengths = [40, 64, 7]
+    p, cap = _filled(lengths, 0, fmt, 22)
+    q = _queries(1, 1, 6, 23)
+    out, lse = _decode(ctx, p, cap, [40, 1000, -5], q, 3, 0.1)
+    _assert_decode(p, cap, [40, 64, 0], q, 3, 0.1, out, lse)
+
+
 def test_decode_of_an_empty_cache(ctx):
     p, cap = _filled([0, 0], 0, Q.E4M3, 1)
     out, lse = _decode(ctx, p, cap, [0, 0], _queries(1, 1, 2, 1), 2, 0.1)

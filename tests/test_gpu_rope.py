@@ -95,6 +95,22 @@ def test_strides_in_place_and_other_streams(ctx, kind, r):
     _assert_close(b, a, pos.numpy(), w, 1.0, True, False)
 
 
+def test_a_broadcast_input_and_offsets_past_32_bits(ctx):
+    w, rot = _rotary(128, False)
+    x = torch.randn((1, 1, 9, 128), generator=torch.Generator().manual_seed(8)).to(torch.bfloat16).cuda()
+    y = torch.empty((3, 4, 9, 128), dtype=torch.bfloat16, device="cuda")
+    lkv.lkv_rope(ctx, rot, x.expand(3, 4, 9, 128), y, first_position=5)
+    _assert_close(y, x.expand(3, 4, 9, 128), 5 + np.arange(9), w, 1.0, False, False)
+    far = (1 << 31) + 64 * 128                                # elements: past 32 bits as an offset, in bytes and in elements
+    store = torch.empty(far + 2 * 40 * 128, dtype=torch.bfloat16, device="cuda")
+    for shape, strides in (((2, 1, 40, 128), (far, 0, 128, 1)), ((1, 2, 40, 128), (0, far, 128, 1)), ((1, 1, 2, 128), (0, 0, far, 1))):
+        v = store.as_strided(shape, strides)
+        v.copy_(torch.randn(shape, generator=torch.Generator().manual_seed(9)))
+        before = v.clone()
+        lkv.lkv_rope(ctx, rot, v, v, first_position=3)
+        _assert_close(v, before, 3 + np.arange(shape[2]), w, 1.0, False, False)
+
+
 @pytest.mark.parametrize("pairs", [False, True])
 def test_far_and_negative_positions(ctx, pairs):
     pos = np.array([0, -1, -2 ** 31, 2 ** 31 - 1, 1 << 20, 123456789, 7, -99999])
@@ -204,6 +220,7 @@ def test_refusals(ctx):
     call(1, a=None); call(1, b=None); call(1, xs=None); call(1, ys=None); call(1, a=C.c_void_p(x.data_ptr() + 2)); call(1, b=C.c_void_p(y.data_ptr() + 8))
     for i in range(3):
         call(1, xs=odd(i, 132)); call(1, ys=odd(i, 4))
+        call(1, ys=odd(i, 0))
     call(1, b=ptr(x), ys=odd(2, 256)); call(1, backward=2); call(1, first=2 ** 31 - 2); call(2, n=(1 << 16, 1, 1 << 15))
     call(1, rotary=bad(layout=3)); call(1, rotary=bad(rotary_dim=0)); call(1, rotary=bad(rotary_dim=7)); call(1, rotary=bad(rotary_dim=256))
     call(1, rotary=bad(inv_freq=None)); call(1, rotary=bad(factor=float("inf")))
