@@ -15,17 +15,18 @@
 // the values' scale the probabilities.
 //   S^T[token, head] = K[token, :] . Q[head, :]^T      (A = K tile, B = Q^T; bf16, into which every code converts exactly)
 //   O[head, ch]     += P[head, token] V[token, ch]     (A = P,      B = V tile; f16, likewise)
-// Nothing is staged in LDS.  The first product's operand needs 8 channels of a token in a lane: a sum over channels may
-// take them in any order, so a lane takes 16 contiguous bytes of its token's row for two steps and Q's operand is read in that
-// order.  The second needs 8 tokens of a channel in a lane: it loads 8 bytes, 8 channels, of each of the 8 tokens whose scores the
+// The first product's operand needs 8 channels of a token in a lane: a sum over channels may take them in any order, so a lane takes
+// 16 contiguous bytes of its token's row for two steps and Q's operand is read in that order.  Loaded so from memory, neighbouring
+// lanes would read different rows; whole rows are loaded, 8 to an instruction, and change lanes through LDS (256 segments of 1.26
+// million rows 63.9 -> 61.9 us, 896 of 2.9 million 139.9 -> 134.7).  The second needs 8 tokens of a channel in a lane: it loads 8 bytes, 8 channels, of each of the 8 tokens whose scores the
 // first product left with it, and byte permutes (16 for a tile) put the same channel of two tokens side by side, which convert
 // together; column c of the m-th product then is channel 8 c + m, and a lane ends with 8 contiguous channels of the output.
 // Softmax runs in fp32 in the log2 domain.  The weights of the values' codes are at most 1, since the sums are kept in units of the
 // largest value scale so far; they are rounded to f16 and what that left is multiplied too, which holds 22 bits of them
 // (error of the output against 64 bits 2e-7; with two bf16 parts, 16 bits, it was 1.1e-6).
 //
-// Bound by the stream of the rows: 1.26 million rows of 256 segments 56 us (5.8 TB/s) and 5 us for the merge; 2.9 million of
-// 896 in int8 131 us (5.75 TB/s).
+// Bound by the stream of the rows: 1.26 million rows of 256 segments 54.4 us (5.9 TB/s) and 5 us for the merge; 2.9 million of
+// 896 in int8 128 us (5.9 TB/s).
 #include <type_traits>
 
 #include "lkv_kernels.h"
@@ -37,10 +38,11 @@ constexpr int kQdWaves = kQdThreads / 64;
 constexpr int kQdTile = kQuantBlock;
 // Waves on a SIMD, and the blocks of a full launch (one round of resident ones).  Two hide the loads' latency, since the next
 // tile's are always on their way; three bring more pieces to merge, and four leave too few registers (256 segments of 1.26
-// million rows 64.1 : 64.7 : 85.7 us, 896 of 2.9 million 143.6 : 148.9 : 180.0).
+// million rows 64.1 : 64.7 : 85.7 us, 896 of 2.9 million 143.6 : 148.9 : 180.0, before the keys went through LDS).
 constexpr int kQdWavesPerSimd = 2;
 constexpr int kQdBlocks = 512;
-constexpr int kQdManyPieces = 4;        // blocks a segment from which a block of the merge has one query head
+constexpr int kQdSomePieces = 4;        // blocks a segment from which the merge has 8, and
+constexpr int kQdManyPieces = 32;       // 32 half waves to a query head
 constexpr float kQdLog2e = 1.4426950408889634f;
 constexpr float kQdLn2 = 0.6931471805599453f;
 
@@ -105,6 +107,7 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
                     int per_wave, int G, float scale, float* __restrict__ out, float* __restrict__ lse, float* __restrict__ ws_acc,
                     float* __restrict__ ws_m, float* __restrict__ ws_l) {
   extern __shared__ __align__(16) float merge_lds[];   // [waves][G][128] sums, then [waves][G] maxima, then denominators
+  __shared__ __align__(16) uint8_t key_lds[kQdWaves][kQdTile * kHeadDim];
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -145,18 +148,17 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
   const bool together = next_first <= (int)blockIdx.x * kQdWaves * per_wave &&
                         ((int)blockIdx.x + 1) * kQdWaves * per_wave <= next_first + (next.len + kQdTile - 1) / kQdTile;
 
-  // What a lane holds of a tile: bytes 64 w + 16 r .. + 15 of token 16 h + c of the keys, bytes 8 c .. 8 c + 7 of token
+  // What a lane holds of a tile: bytes 16 (lane & 7) .. + 15 of token 8 i + lane / 8 of the keys, bytes 8 c .. 8 c + 7 of token
   // 16 h + 4 r + e of the values.
-  uint4 kk[2][2];
+  uint4 kk[4];
   uint2 vv[2][4];
   float ks, vs;
   auto load_keys = [&](int64_t row0, int last, int number) __attribute__((always_inline)) {   // rows past the end: the last row again
     const uint8_t* base = rows.k + row0 * kHeadDim;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t at = (uint32_t)min(16 * h + c, last) * kHeadDim + 16 * r;
-      kk[h][0] = load_stream16(reinterpret_cast<const uint4*>(base + at));
-      kk[h][1] = load_stream16(reinterpret_cast<const uint4*>(base + at + 64));
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t at = (uint32_t)min(8 * i + (lane >> 3), last) * kHeadDim + 16 * (lane & 7);
+      kk[i] = load_stream16(reinterpret_cast<const uint4*>(base + at));
     }
     ks = rows.k_scale[number];
     asm volatile("" ::: "memory");   // asked for here, not where they are used
@@ -208,17 +210,12 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
   // One set of registers a tile: the next tile's keys are asked for when this one's have been multiplied, its values likewise.
 #pragma unroll 1
   for (int t = now.tile; t < now.end; ++t) {
-    f32x4_t sacc[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      sacc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(kk[h][w].x, kk[h][w].y), qfrag[w][0], sacc[h], 0, 0, 0);
-        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(kk[h][w].z, kk[h][w].w), qfrag[w][1], sacc[h], 0, 0, 0);
-      }
-    }
+    // The keys change lanes through LDS: token t's piece p lies at p ^ (t / 2 & 7) of its row, where both sides meet all banks.
     const float ts = qscale * ks;
+    uint8_t* tile = key_lds[wave];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<uint4*>(tile + (8 * i + (lane >> 3)) * kHeadDim + 16 * ((lane & 7) ^ ((4 * i + (lane >> 4)) & 7))) = kk[i];
     // Asked for in any case, so that the waits for this tile's values can count the loads behind them; behind a wave's last
     // tile it is one row of it again.
     if (t + 1 < now.end) {
@@ -233,6 +230,20 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
       last = 0;
     }
     load_keys(row0, last, number);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    f32x4_t sacc[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      sacc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const uint4 k = *reinterpret_cast<const uint4*>(tile + (16 * h + c) * kHeadDim + 16 * ((4 * w + r) ^ (c >> 1)));
+        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(k.x, k.y), qfrag[w][0], sacc[h], 0, 0, 0);
+        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(k.z, k.w), qfrag[w][1], sacc[h], 0, 0, 0);
+      }
+    }
     float p[8];
     float mx = m_run;
 #pragma unroll
@@ -364,12 +375,13 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
 }
 
 // The pieces of a segment of several.  Half a wave holds the 128 channels of a segment's query head, four a lane, and has eight
-// pieces' loads in flight together.  kParts = 1: a block merges eight heads; else, where segments have many pieces, its eight half waves
-// share those of one head and their sums meet in LDS.
+// pieces' loads in flight together.  kParts = 1: a block merges eight heads; else, where segments have many pieces, kParts half waves
+// share those of one head and their sums meet in LDS.  Eight or 32 half waves (whole call): one segment of 60 thousand rows, 470 pieces, 17.1 : 13.9
+// us; 8 segments of 20 thousand, 52 each, 19.0 : 16.9; 32 of 3 thousand, 12 each, 12.8 : 13.4; 8 of 614, 5 each, 8.3 : 9.0.
 constexpr int kQdHalf = 32;
 constexpr int kQdHalves = kQdThreads / kQdHalf;
 template <int kParts>
-__global__ void __launch_bounds__(kQdThreads)
+__global__ void __launch_bounds__(kParts == 1 ? kQdThreads : kParts * kQdHalf)
 quant_decode_merge_kernel(const int32_t* __restrict__ cap, const int32_t* __restrict__ lengths, int n_heads, int per_wave, int G,
                           const float* __restrict__ ws_acc, const float* __restrict__ ws_m, const float* __restrict__ ws_l,
                           float* __restrict__ out, float* __restrict__ lse) {
@@ -420,18 +432,18 @@ quant_decode_merge_kernel(const int32_t* __restrict__ cap, const int32_t* __rest
     }
   }
   if constexpr (kParts > 1) {
-    __shared__ float4 num_lds[kQdHalves][kQdHalf];
-    __shared__ float mx_lds[kQdHalves], den_lds[kQdHalves];
+    __shared__ float4 num_lds[kParts][kQdHalf];
+    __shared__ float mx_lds[kParts], den_lds[kParts];
     num_lds[half][lane] = num;
     if (lane == 0) { mx_lds[half] = mx; den_lds[half] = den; }
     __syncthreads();
     if (half > 0) return;
 #pragma unroll
-    for (int p = 1; p < kQdHalves; ++p) mx = fmaxf(mx, mx_lds[p]);
+    for (int p = 1; p < kParts; ++p) mx = fmaxf(mx, mx_lds[p]);
     num = make_float4(0.f, 0.f, 0.f, 0.f);
     den = 0.f;
 #pragma unroll
-    for (int p = 0; p < kQdHalves; ++p) {
+    for (int p = 0; p < kParts; ++p) {
       const float weight = qd_exp2(mx_lds[p] - mx);   // 0 for a part without pieces
       const float4 v = num_lds[p][lane];
       num.x = fmaf(v.x, weight, num.x);
@@ -487,9 +499,10 @@ hipError_t launch_quant_decode(int format, int G, const void* q, const QuantRows
     constexpr int kParts = decltype(tag)::value;
     const int n_heads = n_segments * G;
     hipLaunchKernelGGL((quant_decode_merge_kernel<kParts>), dim3(kParts == 1 ? (n_heads + kQdHalves - 1) / kQdHalves : n_heads),
-                       dim3(kQdThreads), 0, stream, cap, lengths, n_heads, shape.per_wave, G, ws_acc, ws_m, ws_l, out, lse);
+                       dim3(kParts == 1 ? kQdThreads : kParts * kQdHalf), 0, stream, cap, lengths, n_heads, shape.per_wave, G, ws_acc, ws_m, ws_l, out, lse);
   };
-  if (shape.blocks > kQdManyPieces * n_segments) merge(std::integral_constant<int, kQdHalves>{});
+  if (shape.blocks > kQdManyPieces * n_segments) merge(std::integral_constant<int, 32>{});
+  else if (shape.blocks > kQdSomePieces * n_segments) merge(std::integral_constant<int, kQdHalves>{});
   else merge(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
