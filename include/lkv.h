@@ -24,14 +24,16 @@
  *           caller has synchronised the stream.  Calls that only enqueue kernels
  *           can be recorded into a HIP graph.  The one exception is an upload
  *           of segment offsets computed from HOST budgets: lkv_plan_offsets,
- *           lkv_reevict, and lkv_select when it is given host budgets for 640
- *           or more segments (fewer travel in the kernel arguments).  Such an
- *           upload goes through a ring of 8 pinned buffers owned by the
- *           context, may wait on the host until the ring slot's previous
- *           upload has finished, and is refused with LKV_ERR_UNSUPPORTED while
- *           `stream` is capturing (a replay would copy whatever a later call
- *           left in the slot).  To stay free of both, call lkv_plan_offsets
- *           once, outside any capture, and pass budgets = NULL to lkv_select.
+ *           and lkv_select, lkv_reevict and lkv_reevict_quant when given host
+ *           budgets for 640 or more segments (fewer travel in the kernel
+ *           arguments).  Such an upload goes through a ring of 8 pinned
+ *           buffers owned by the context, may wait on the host until the ring
+ *           slot's previous upload has finished, and is refused with
+ *           LKV_ERR_UNSUPPORTED while `stream` is capturing (a replay would
+ *           copy whatever a later call left in the slot).  To stay free of
+ *           both, call lkv_plan_offsets once, outside any capture, and pass
+ *           budgets = NULL to lkv_select.  The two re-evictions are refused in
+ *           a capture at any size: a replay would use the old budgets.
  * Layout.   Cache tensors are bf16, row-major [n_layers, n_kv_heads, T, 128]
  *           per sequence.  A "segment" is one (sequence, layer, kv head); the
  *           segments are numbered s = (seq * n_layers + layer) * n_kv_heads +

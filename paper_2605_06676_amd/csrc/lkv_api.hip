@@ -630,14 +630,32 @@ lkv_status check_reeviction(lkv_ctx* ctx, int64_t n_segments, int32_t head_dim, 
 // Row numbers that a re-eviction keeps of every segment, and the tight offsets of the new budgets that they are written at.
 lkv_status reevict_select(lkv_ctx* ctx, int64_t n_segments, const int32_t* new_budgets, int max_len, const float* up,
                           const int32_t* cap_offsets, const int32_t* lengths, int32_t* idx, int32_t* offsets, void* stream) {
-  if (lkv_status st = lkv_plan_offsets(ctx, n_segments, new_budgets, offsets, nullptr, stream)) return st;
+  // few segments' offsets travel in the kernel arguments, as lkv_select's do; refused in a capture either way, since the budgets
+  // follow the caller's count of the rows and a replay would use the old ones
+  int32_t host_off[1024];
+  const bool inline_offsets = n_segments < lkv::select_inline_capacity();
+  if (inline_offsets) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    if (hipError_t e = hipStreamIsCapturing(as_stream(stream), &cap)) return hip_fail(ctx, e, "capture status query");
+    if (cap != hipStreamCaptureStatusNone)
+      return fail(ctx, LKV_ERR_UNSUPPORTED, "a re-eviction takes its budgets from host memory and cannot be captured into a HIP graph");
+    int32_t run = 0;
+    for (int64_t i = 0; i < n_segments; ++i) {
+      host_off[i] = run;
+      run += new_budgets[i];
+    }
+    host_off[n_segments] = run;
+  } else if (lkv_status st = lkv_plan_offsets(ctx, n_segments, new_budgets, offsets, nullptr, stream)) {
+    return st;
+  }
   lkv::SeqTable tab;
   memset(&tab, 0, sizeof(tab));
   tab.T[0] = max_len;          // upper bound of every segment's length: sizes the LDS region
   tab.first[0] = 0;
   tab.first[1] = (int32_t)n_segments;
   tab.n = 1;
-  lkv::launch_select(tab, nullptr, (int)n_segments, offsets, idx, 0, 0, as_stream(stream), up, cap_offsets, lengths);
+  lkv::launch_select(tab, inline_offsets ? host_off : nullptr, (int)n_segments, offsets, idx, 0, 0, as_stream(stream), up, cap_offsets,
+                     lengths);
   if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "re-eviction select launch");
   return LKV_OK;
 }
@@ -925,10 +943,6 @@ lkv_status lkv_compact_quant(lkv_ctx* ctx, const lkv_cache* cache, const float* 
   for (int s = 0; up != nullptr && s < cache->n_seq; ++s)
     if (scores[s] == nullptr) return fail(ctx, LKV_ERR_INVALID_ARG, "scores[%d] is NULL", s);
   hipStream_t st = as_stream(stream);
-  if (cap_offsets != nullptr) {
-    lkv::launch_grown_layout(offsets, (int)n_seg, slack, cap_offsets, lengths, st);
-    if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_compact_quant layout launch");
-  }
   for (int s0 = 0; s0 < cache->n_seq; s0 += lkv::kMaxSeqPerLaunch) {
     lkv::SeqTable tab;
     memset(&tab, 0, sizeof(tab));
@@ -940,7 +954,8 @@ lkv_status lkv_compact_quant(lkv_ctx* ctx, const lkv_cache* cache, const float* 
       tab.T[i] = cache->seq_len[s0 + i];
     }
     tab.n = n;
-    lkv::launch_quant_compact(tab, packed->format, idx, offsets, (int)n_seg, heads, s0, total_kept, slack, as_quant_rows(packed), up, st);
+    lkv::launch_quant_compact(tab, packed->format, idx, offsets, (int)n_seg, heads, s0, total_kept, slack, as_quant_rows(packed), up,
+                              cap_offsets, lengths, st);
     if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_compact_quant launch");
   }
   return LKV_OK;
@@ -1021,10 +1036,9 @@ lkv_status lkv_reevict_quant(lkv_ctx* ctx, int64_t n_segments, int32_t head_dim,
   if (lkv_status st = reevict_select(ctx, n_segments, new_budgets, max_len, up, cap_offsets, lengths, idx, offsets, stream)) return st;
   hipStream_t st = as_stream(stream);
   lkv::launch_quant_recompact(packed->format, idx, offsets, (int)n_segments, total, slack,
-                              lkv::QuantOld{as_quant_rows(packed), up, cap_offsets, lengths}, as_quant_rows(packed_new), up_new, st);
+                              lkv::QuantOld{as_quant_rows(packed), up, cap_offsets, lengths}, as_quant_rows(packed_new), up_new,
+                              cap_offsets_new, lengths_new, st);
   if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_reevict_quant compact launch");
-  lkv::launch_grown_layout(offsets, (int)n_segments, slack, cap_offsets_new, lengths_new, st);
-  if (hipError_t e = hipGetLastError()) return hip_fail(ctx, e, "lkv_reevict_quant layout launch");
   if (total_kept != nullptr) *total_kept = total;
   return LKV_OK;
 }

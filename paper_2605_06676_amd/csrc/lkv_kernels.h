@@ -96,9 +96,10 @@ struct QuantOld {   // the packed 8-bit cache that a re-eviction reads
 };
 void launch_quant_compact(const SeqTable& tab, int format, const int32_t* idx, const int32_t* offsets, int n_segments,
                           int heads_per_seq, int seq_lo, int64_t total_kept, int slack, const QuantRows& dst, float* up,
-                          hipStream_t stream);
+                          int32_t* cap_out, int32_t* len_out, hipStream_t stream);
 void launch_quant_recompact(int format, const int32_t* idx, const int32_t* offsets, int n_segments, int64_t total_kept, int slack,
-                            const QuantOld& old, const QuantRows& dst, float* up, hipStream_t stream);
+                            const QuantOld& old, const QuantRows& dst, float* up, int32_t* cap_out, int32_t* len_out,
+                            hipStream_t stream);
 
 // quant_append.hip
 struct AppendScorer {   // w1 null: no scores

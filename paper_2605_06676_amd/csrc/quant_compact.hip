@@ -113,7 +113,8 @@ __device__ __forceinline__ float requant_block(const uint2 (&x)[kQcLoads], const
 template <int kFormat, bool kPacked>
 __global__ void __launch_bounds__(kQcThreads)
 quant_compact_kernel(SeqTable tab, const int32_t* __restrict__ idx, const int32_t* __restrict__ offsets, int n_segments,
-                     int heads_per_seq, int seq_lo, int slack, QuantRows dst, float* __restrict__ up, QuantOld old) {
+                     int heads_per_seq, int seq_lo, int slack, QuantRows dst, float* __restrict__ up, int32_t* __restrict__ cap_out,
+                     int32_t* __restrict__ len_out, QuantOld old) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   auto first_scale = [&](int s) { return quant_first_scale(offsets[s] + slack * s, s); };
@@ -125,6 +126,11 @@ quant_compact_kernel(SeqTable tab, const int32_t* __restrict__ idx, const int32_
   const int o = offsets[s], len = offsets[s + 1] - o;
   const int cap = o + slack * s;
   const int64_t ahead = (int64_t)(number - quant_first_scale(cap, s)) * kQuantBlock;   // rows of the segment ahead of the block
+  if (ahead == 0 && lane == 0 && cap_out != nullptr) {   // a segment always has its first number
+    cap_out[s] = cap;
+    len_out[s] = len;
+    if (s == n_segments - 1) cap_out[n_segments] = cap + len + slack;
+  }
   if (ahead >= len) return;   // a number without rows; the whole wave
   const int first = (int)ahead;
   const int n = min(len - first, kQuantBlock);
@@ -190,32 +196,34 @@ quant_compact_kernel(SeqTable tab, const int32_t* __restrict__ idx, const int32_
 template <bool kPacked>
 static void launch_quant_compact_any(const SeqTable& tab, int format, const int32_t* idx, const int32_t* offsets, int n_segments,
                                      int heads_per_seq, int seq_lo, int64_t total_kept, int slack, const QuantRows& dst, float* up,
-                                     const QuantOld& old, int n_own, hipStream_t stream) {
-  if (total_kept <= 0) return;
+                                     int32_t* cap_out, int32_t* len_out, const QuantOld& old, int n_own, hipStream_t stream) {
+  if (total_kept <= 0 && cap_out == nullptr) return;
   // block numbers of n_own segments over at most the rows of the whole cache
   const int64_t numbers = (total_kept + (int64_t)n_segments * slack) / kQuantBlock + n_own + 1;
   const dim3 grid((unsigned)((numbers + kQcWaves - 1) / kQcWaves));
   if (format == kQuantE4m3)
     hipLaunchKernelGGL((quant_compact_kernel<kQuantE4m3, kPacked>), grid, dim3(kQcThreads), 0, stream, tab, idx, offsets, n_segments,
-                       heads_per_seq, seq_lo, slack, dst, up, old);
+                       heads_per_seq, seq_lo, slack, dst, up, cap_out, len_out, old);
   else
     hipLaunchKernelGGL((quant_compact_kernel<kQuantInt8, kPacked>), grid, dim3(kQcThreads), 0, stream, tab, idx, offsets, n_segments,
-                       heads_per_seq, seq_lo, slack, dst, up, old);
+                       heads_per_seq, seq_lo, slack, dst, up, cap_out, len_out, old);
 }
 
 void launch_quant_compact(const SeqTable& tab, int format, const int32_t* idx, const int32_t* offsets, int n_segments,
                           int heads_per_seq, int seq_lo, int64_t total_kept, int slack, const QuantRows& dst, float* up,
-                          hipStream_t stream) {
+                          int32_t* cap_out, int32_t* len_out, hipStream_t stream) {
   QuantOld none = {};
-  launch_quant_compact_any<false>(tab, format, idx, offsets, n_segments, heads_per_seq, seq_lo, total_kept, slack, dst, up, none,
-                                  tab.n * heads_per_seq, stream);
+  launch_quant_compact_any<false>(tab, format, idx, offsets, n_segments, heads_per_seq, seq_lo, total_kept, slack, dst, up, cap_out,
+                                  len_out, none, tab.n * heads_per_seq, stream);
 }
 
 void launch_quant_recompact(int format, const int32_t* idx, const int32_t* offsets, int n_segments, int64_t total_kept, int slack,
-                            const QuantOld& old, const QuantRows& dst, float* up, hipStream_t stream) {
+                            const QuantOld& old, const QuantRows& dst, float* up, int32_t* cap_out, int32_t* len_out,
+                            hipStream_t stream) {
   SeqTable tab;
   memset(&tab, 0, sizeof(tab));
-  launch_quant_compact_any<true>(tab, format, idx, offsets, n_segments, 1, 0, total_kept, slack, dst, up, old, n_segments, stream);
+  launch_quant_compact_any<true>(tab, format, idx, offsets, n_segments, 1, 0, total_kept, slack, dst, up, cap_out, len_out, old, n_segments,
+                                 stream);
 }
 
 }  // namespace lkv

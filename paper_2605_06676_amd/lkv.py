@@ -602,14 +602,16 @@ class QuantRows:
     def __init__(self, k, v, k_scale, v_scale):
         import torch
 
-        assert k.dtype == v.dtype and k.dtype in (torch.float8_e4m3fn, torch.int8)
-        assert k.dim() == 2 and k.shape[1] == 128 and k.shape == v.shape
-        assert k_scale.dtype == torch.float32 and v_scale.dtype == torch.float32 and k_scale.numel() == v_scale.numel()
-        for t in (k, v, k_scale, v_scale):
-            assert t.is_cuda and t.is_contiguous()
+        kind, shape, scales = k.dtype, k.shape, k_scale.numel()
+        assert kind is torch.int8 or kind is torch.float8_e4m3fn
+        assert len(shape) == 2 and shape[1] == 128 and v.dtype is kind and v.shape == shape
+        assert k_scale.dtype is torch.float32 and v_scale.dtype is torch.float32 and v_scale.numel() == scales
+        assert k.is_cuda and v.is_cuda and k_scale.is_cuda and v_scale.is_cuda
+        assert k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.rows, self.scales = int(k.shape[0]), int(k_scale.numel())
-        self.c = _QuantRows(QUANT_INT8 if k.dtype == torch.int8 else QUANT_E4M3, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+        self.rows, self.scales = shape[0], scales
+        self.c = _QuantRows(QUANT_INT8 if kind is torch.int8 else QUANT_E4M3, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+                            v_scale.data_ptr())
 
     def _check(self, n_segments: int, rows: int):
         """What the library cannot see from pointers: that the tensors hold a cache of this size."""
@@ -647,7 +649,9 @@ def lkv_append_quant(ctx: Context, n_seq: int, L: int, H: int, d: int, k_new, v_
     """k_new, v_new: bf16 [n_seq, L, H, 128]; positions: GPU int32 [n_seq] with rotary; scorer and up: both or neither."""
     import torch
 
-    assert all(t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == n_seq * L * H * d for t in (k_new, v_new))
+    n = n_seq * L * H * d
+    assert k_new.dtype is torch.bfloat16 and k_new.numel() == n and k_new.is_contiguous()
+    assert v_new.dtype is torch.bfloat16 and v_new.numel() == n and v_new.is_contiguous()
     assert positions is None or (positions.dtype == torch.int32 and positions.numel() == n_seq and positions.is_contiguous())
     sc = None if scorer is None else C.byref(_scorer_struct(scorer))
     ctx._check(ctx.lib.lkv_append_quant(ctx.h, n_seq, L, H, d, sc, None if rotary is None else C.byref(rotary.c), _ptr(positions),
@@ -705,17 +709,19 @@ def lkv_rope(ctx: Context, rotary: Rotary, x, y, positions=None, first_position:
     be x.  positions: GPU int32 [batch, tokens], or [tokens] for all batches, or None: first_position + t."""
     import torch
 
-    assert x.shape == y.shape and x.dtype == y.dtype and x.dtype in (torch.bfloat16, torch.float32) and x.dim() in (3, 4)
-    assert x.is_cuda and y.is_cuda and x.stride(-1) == 1 and y.stride(-1) == 1
-    B, Hn, T, d = x.shape if x.dim() == 4 else (1, *x.shape)
+    kind, shape, sx, sy = x.dtype, x.shape, x.stride(), y.stride()
+    assert (kind is torch.bfloat16 or kind is torch.float32) and y.dtype is kind and y.shape == shape and len(shape) in (3, 4)
+    assert x.is_cuda and y.is_cuda and sx[-1] == 1 and sy[-1] == 1
+    B, Hn, T, d = shape if len(shape) == 4 else (1, *shape)
     # the stride of a single batch, head or token is never followed
-    sx, sy = x.stride(), y.stride()
     xs = _Strides(sx[0] if B > 1 else 0, sx[-3] if Hn > 1 else 0, sx[-2] if T > 1 else 0)
     ys = _Strides(sy[0] if B > 1 else 0, sy[-3] if Hn > 1 else 0, sy[-2] if T > 1 else 0)
-    step = 0
+    step = at = 0
     if positions is not None:
-        assert positions.dtype == torch.int32 and positions.is_cuda and positions.shape[-1] == T and (T == 1 or positions.stride(-1) == 1)
-        assert positions.dim() == 1 or positions.shape == (B, T)
-        step = positions.stride(0) if positions.dim() == 2 and B > 1 else 0
-    ctx._check(ctx.lib.lkv_rope(ctx.h, C.byref(rotary.c), 1 if x.dtype == torch.float32 else 0, B, Hn, T, d, _ptr(x), xs,
-                                _ptr(y), ys, _ptr(positions), step, int(first_position), int(backward), _stream_ptr(stream)))
+        at, rows, steps = positions.data_ptr(), positions.shape, positions.stride()
+        assert positions.dtype is torch.int32 and positions.is_cuda and rows[-1] == T and (T == 1 or steps[-1] == 1)
+        if len(rows) > 1:
+            assert len(rows) == 2 and rows[0] == B
+            step = steps[0] if B > 1 else 0
+    ctx._check(ctx.lib.lkv_rope(ctx.h, C.byref(rotary.c), 1 if kind is torch.float32 else 0, B, Hn, T, d, x.data_ptr(), xs,
+                                y.data_ptr(), ys, at or None, step, int(first_position), int(backward), _stream_ptr(stream)))
