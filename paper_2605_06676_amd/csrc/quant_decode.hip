@@ -22,8 +22,10 @@
 // first product left with it, and byte permutes (16 for a tile) put the same channel of two tokens side by side, which convert
 // together; column c of the m-th product then is channel 8 c + m, and a lane ends with 8 contiguous channels of the output.
 // Softmax runs in fp32 in the log2 domain.  The weights of the values' codes are at most 1, since the sums are kept in units of the
-// largest value scale so far; they are rounded to f16 and what that left is multiplied too, which holds 22 bits of them
-// (error of the output against 64 bits 2e-7; with two bf16 parts, 16 bits, it was 1.1e-6).
+// largest value scale so far; times 2^15 they are rounded to f16 and what that left is multiplied too, which holds 22 bits of them,
+// fewer only below 2^-18 of the largest one, where the step of 2^-39 weighs in
+// (error of the output against 64 bits 2e-7; with two bf16 parts, 16 bits, it was 1.1e-6; without the 2^15, an output that fifty thousand weights of
+// e^-18 make up was off by 6e-4).
 //
 // Bound by the stream of the rows: 1.26 million rows of 256 segments 54.4 us (5.9 TB/s) and 5 us for the merge; 2.9 million of
 // 896 in int8 128 us (5.9 TB/s).
@@ -43,6 +45,7 @@ constexpr int kQdWavesPerSimd = 2;
 constexpr int kQdBlocks = 512;
 constexpr int kQdSomePieces = 4;        // blocks a segment from which the merge has 8, and
 constexpr int kQdManyPieces = 32;       // 32 half waves to a query head
+constexpr float kQdWeightUnit = 32768.f;   // weights of at most 1 times this: f16 holds steps of 2^-24, so 2^-39 of the largest weight
 constexpr float kQdLog2e = 1.4426950408889634f;
 constexpr float kQdLn2 = 0.6931471805599453f;
 
@@ -199,7 +202,7 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
   const QdPiece now = next;
   float m_run = -INFINITY, l_run = 0.f;   // running maximum of head c (log2 domain) in its four lanes, this lane's share of the denominator
   float vs_run = 0.f;                     // largest value scale so far: the sums are in units of it
-  f32x4_t acc[8];                         // O[head 4 r + e][channel 8 c + m]
+  f32x4_t acc[8];                         // O[head 4 r + e][channel 8 c + m], in units of vs_run / kQdWeightUnit
 #pragma unroll
   for (int m = 0; m < 8; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   next = next_piece(now.s + 1);   // while the rows are on their way
@@ -264,10 +267,10 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
     l_run = l_run * alpha + psum;
     const float vs_new = fmaxf(vs_run, vs);
     const float unit = vs_new > 0.f ? 1.f / vs_new : 0.f;
-    const float ratio = vs * unit;
+    const float ratio = vs * unit * kQdWeightUnit;
     alpha *= vs_run * unit;
     vs_run = vs_new;
-    f16x8_t phigh, plow;   // the weights of the values' codes, at most 1: rounded to f16, and what the rounding left
+    f16x8_t phigh, plow;   // the weights of the values' codes, at most kQdWeightUnit: rounded to f16, and what the rounding left
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float w = p[i] * ratio;
@@ -317,7 +320,7 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
 #pragma unroll
   for (int m = 0; m < 8; ++m)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[m][e] *= vs_run;
+    for (int e = 0; e < 4; ++e) acc[m][e] *= vs_run * (1.f / kQdWeightUnit);
   if (next.s >= 0) load_q(next);
   l_run = sum_over_row_blocks(l_run);
   if (together) {   // the only piece of each wave

@@ -272,6 +272,27 @@ def test_decode_with_scales_of_any_kind(ctx, fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("ahead", [0.0, 3.0, 10.5, 14.0, 18.0])
+def test_decode_of_one_large_weight_and_many_small_ones(ctx, fmt, ahead):
+    """One row is `ahead` in its score and has value 0, fifty thousand have score 0 and value 1: what the output holds comes from
+    weights of e^-ahead.  All terms are positive, so the sums are off by their depth: 32 rows of a tile, 4 waves, 13 and 32 pieces,
+    100 * 2^-24, and a weight by 2^-20 (exp2 of an argument up to 26, 22 bits of the weight)."""
+    n = 50000
+    p = Packed(n, 1, fmt)
+    k, v = np.zeros((n, 128)), np.ones((n, 128))
+    k[77, 3], v[77] = 1.0, 0.0
+    Q.write_segment(k, 0, 0, p.kc, p.ks, fmt)
+    Q.write_segment(v, 0, 0, p.vc, p.vs, fmt)
+    p.upload()
+    q = torch.zeros((1, 1, 2, 128), dtype=torch.bfloat16)
+    q[..., 3] = 1.0
+    out, lse = _decode(ctx, p, [0, n], [n], q, 1, ahead)
+    rest = (n - 1) * np.exp(-ahead)
+    assert np.abs(out / (rest / (1 + rest)) - 1).max() <= 100 * 2.0 ** -24 + 2.0 ** -20
+    assert np.abs(lse - (ahead + np.log1p(rest))).max() <= 100 * 2.0 ** -24 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_decode_reads_nothing_of_spare_rows(ctx, fmt):
     lengths = [70, 0, 31]
     p, cap = _filled(lengths, 40, fmt, 15)
