@@ -11,7 +11,8 @@
 // Blocks follow memory: those that run together lie together, whichever of heads and tokens is the inner one.  With the heads inside
 // where the tokens are, strides of a power of two put the rows in flight on few channels: 32 heads of 16384 tokens in bf16 59.4 us, 53.9 (5.0
 // TB/s) so; 32 of 8192 in fp32 73.6 and 51.2; but 32 batches of 32 heads of 512 tokens 50.0 and 63.3, which the batches outside mend.
-// Few heads leave the cosines as the bound: one head of 524288 tokens 105 us.
+// Few heads leave the cosines as the bound (one head of 524288 tokens 102 us), and halves that are no whole lines the stores (96
+// channels turned 62 us; with stores that meet in the caches 61, but 128 channels 62 and not 56).
 #include <type_traits>
 
 #include "lkv_kernels.h"
@@ -48,9 +49,21 @@ template <typename T> __device__ __forceinline__ T rope_put(float f) {
   else return f;
 }
 
-// kWide: the rotated channels of either half are whole pieces (rotary_dim a multiple of 16 in bf16 and of 8 in fp32).  Else
-// a lane takes one pair at a time.
-template <typename T, bool kWide>
+// Of a piece that starts with pair `first`, the words of turned pairs, and the others as they were.
+template <typename T>
+__device__ __forceinline__ uint4 rope_blend(const uint4& turned, const uint4& raw, int first, int n_pairs) {
+  constexpr int kWords = (int)sizeof(T) / 2;   // of a pair
+  return make_uint4(first < n_pairs ? turned.x : raw.x, first + 1 / kWords < n_pairs ? turned.y : raw.y,
+                    first + 2 / kWords < n_pairs ? turned.z : raw.z, first + 3 / kWords < n_pairs ? turned.w : raw.w);
+}
+
+// How a lane has its pairs.  kRopeNeighbours: channels 2 i and 2 i + 1, any rotary_dim.  kRopeHalves: halves of whole pieces (rotary_dim
+// a multiple of 16 in bf16 and of 8 in fp32).  kRopeSingle: other halves, one pair at a time (32 heads of 16384 tokens, 34 channels
+// turned: 86 us, as neighbours 53).
+constexpr int kRopeNeighbours = 0;
+constexpr int kRopeHalves = 1;
+constexpr int kRopeSingle = 2;
+template <typename T, int kLayout>
 __global__ void __launch_bounds__(kRopeThreads)
 rope_kernel(RotaryArgs rot, const T* x, RopeStrides xs, T* y, RopeStrides ys, const int32_t* __restrict__ positions,
             int64_t positions_stride, int first_position, uint32_t n_tokens, uint32_t run /* rows that a block may join */, int n_heads,
@@ -81,7 +94,7 @@ rope_kernel(RotaryArgs rot, const T* x, RopeStrides xs, T* y, RopeStrides ys, co
   };
 
   const int wave = tid >> 6, lane = tid & 63;
-  if constexpr (kWide) {
+  if constexpr (kLayout != kRopeSingle) {
     constexpr int kPiece = 16 / (int)sizeof(T);              // elements
     constexpr int kLanes = kHeadDim / (2 * kPiece);          // of a row
     constexpr int kRows = 64 / kLanes;                       // of a wave's load
@@ -90,14 +103,13 @@ rope_kernel(RotaryArgs rot, const T* x, RopeStrides xs, T* y, RopeStrides ys, co
     const int each = (heads * groups + kRopeWaves - 1) / kRopeWaves;
     const int item0 = wave * each, item1 = min(item0 + each, heads * groups);
     const int at = lane % kLanes;
-    // this lane's two pieces, and whether they are turned: with each other (halves) or in themselves (pairs)
-    const bool halves = rot.pairs == 0;
+    // this lane's two pieces, which are turned with each other (halves) or in themselves (pairs)
+    constexpr bool halves = kLayout == kRopeHalves;
     const int turned_lanes = half / kPiece;                  // halves: lanes of rotated channels; the others share the rest likewise
-    const bool turned0 = halves ? at < turned_lanes : at * kPiece < rot.rotary_dim;
-    const bool turned1 = halves ? turned0 : kRopePairs + at * kPiece < rot.rotary_dim;
+    const bool turned = at < turned_lanes;
     const int rest = rot.rotary_dim + (at - turned_lanes) * kPiece;
-    const int ch0 = !halves ? at * kPiece : turned0 ? at * kPiece : rest;
-    const int ch1 = !halves ? kRopePairs + at * kPiece : turned0 ? half + at * kPiece : rest + (kHeadDim - rot.rotary_dim) / 2;
+    const int ch0 = !halves || turned ? at * kPiece : rest;
+    const int ch1 = !halves ? kRopePairs + at * kPiece : turned ? half + at * kPiece : rest + (kHeadDim - rot.rotary_dim) / 2;
     uint4 p0[kRopeUnroll], p1[kRopeUnroll];
     int64_t out[kRopeUnroll];   // where a row goes, -1: nowhere
     int token[kRopeUnroll];
@@ -139,16 +151,24 @@ rope_kernel(RotaryArgs rot, const T* x, RopeStrides xs, T* y, RopeStrides ys, co
             rotary_turn(f1[2 * i], f1[2 * i + 1], c[kRopePairs / 2 + pair], s[kRopePairs / 2 + pair]);
           }
         }
-        if (out[u] >= 0) {   // a piece that is not turned goes bit for bit
-          store_stream16(reinterpret_cast<uint4*>(y + out[u] + ch0), turned0 ? rope_pack(f0) : p0[u]);
-          store_stream16(reinterpret_cast<uint4*>(y + out[u] + ch1), turned1 ? rope_pack(f1) : p1[u]);
+        if (out[u] < 0) continue;
+        const uint4 t0 = rope_pack(f0), t1 = rope_pack(f1);   // what is not turned goes bit for bit
+        uint4 w0, w1;
+        if (halves) {
+          w0 = turned ? t0 : p0[u];
+          w1 = turned ? t1 : p1[u];
+        } else {
+          w0 = rope_blend<T>(t0, p0[u], at * (kPiece / 2), half);
+          w1 = rope_blend<T>(t1, p1[u], kRopePairs / 2 + at * (kPiece / 2), half);
         }
+        store_stream16(reinterpret_cast<uint4*>(y + out[u] + ch0), w0);
+        store_stream16(reinterpret_cast<uint4*>(y + out[u] + ch1), w1);
       }
     }
   } else {
     fill_tables();
-    const int ch0 = lane < half && rot.pairs == 0 ? lane : 2 * lane;
-    const int ch1 = lane < half && rot.pairs == 0 ? lane + half : 2 * lane + 1;
+    const int ch0 = lane < half ? lane : 2 * lane;
+    const int ch1 = lane < half ? lane + half : 2 * lane + 1;
     // y may be x: a round's loads go ahead of its stores by hand
     for (int i0 = wave; i0 < heads * tokens; i0 += kRopeWaves * kRopeUnroll) {
       T x0[kRopeUnroll], x1[kRopeUnroll];
@@ -185,15 +205,18 @@ void launch_rope(const RotaryArgs& rot, bool f32, const void* x, const RopeStrid
   const uint32_t blocks = n_rows / run * ((run + kRopeTokens - 1) / kRopeTokens);
   const uint32_t head_blocks = (uint32_t)(n_heads + kRopeHeads - 1) / kRopeHeads;
   const bool heads_inside = xs.head < xs.token;
-  auto launch = [&](auto tag, auto wide) {
+  auto launch = [&](auto tag, auto layout) {
     using T = decltype(tag);
-    hipLaunchKernelGGL((rope_kernel<T, decltype(wide)::value>), dim3(blocks * head_blocks), dim3(kRopeThreads), 0, stream, rot,
+    hipLaunchKernelGGL((rope_kernel<T, decltype(layout)::value>), dim3(blocks * head_blocks), dim3(kRopeThreads), 0, stream, rot,
                        static_cast<const T*>(x), xs, static_cast<T*>(y), ys, positions, positions_stride, first_position,
                        (uint32_t)n_tokens, run, n_heads, head_blocks, heads_inside, backward ? -1.f : 1.f);
   };
-  const bool wide = rot.rotary_dim % (f32 ? 8 : 16) == 0;
-  if (f32) { if (wide) launch(float{}, std::true_type{}); else launch(float{}, std::false_type{}); }
-  else { if (wide) launch(uint16_t{}, std::true_type{}); else launch(uint16_t{}, std::false_type{}); }
+  auto launch_layout = [&](auto tag) {
+    if (rot.pairs != 0) launch(tag, std::integral_constant<int, kRopeNeighbours>{});
+    else if (rot.rotary_dim % (int)(32 / sizeof(tag)) == 0) launch(tag, std::integral_constant<int, kRopeHalves>{});
+    else launch(tag, std::integral_constant<int, kRopeSingle>{});
+  };
+  if (f32) launch_layout(float{}); else launch_layout(uint16_t{});
 }
 
 }  // namespace lkv
