@@ -378,7 +378,8 @@ lkv_status lkv_reevict(lkv_ctx *ctx, int64_t n_segments, int32_t head_dim, const
  * offsets, slack and growth are those of the bf16 cache above.  Every LKV_QUANT_BLOCK = 32 rows of a segment, counted from its
  * first row, are a block with one fp32 scale for their keys and one for their values: value = code * scale.
  *   LKV_QUANT_E4M3 : codes are 8-bit floating-point numbers (4 exponent and 3 mantissa bits, no infinities, largest 448):
- *                    relative error up to 2^-4, whatever else is in the block; the choice for keys with outlier channels
+ *                    relative error up to 2^-4, whatever else is in the block: the choice where a few channels are far above the others
+ *                    (more than ten times)
  *   LKV_QUANT_INT8 : codes are whole numbers in [-127, 127]: error up to half a scale, i.e. up to 1/127 of the block's
  *                    largest magnitude; two to three times as exact as e4m3 for values of one size
  * A scale is the smallest power of two s with max |value| <= 448 s (127 s), at least 2^-126, and 0 for a block of zeros; a code
