@@ -468,6 +468,7 @@ typedef struct {
 lkv_status lkv_rope_frequencies(const lkv_rope_scaling *scaling, double *inv_freq, double *factor);
 
 /* Rotates [n_batch, n_heads, n_tokens, 128] of any strides with the channels contiguous.
+ * Sizes: n_batch * n_tokens < 2^31, and fewer than 2^24 blocks of 32 tokens of 4 heads.
  * dtype      : of x and y: LKV_BF16 (q, k) or LKV_FP32 (their gradients as lkv_masked_attn_backward writes them); the
  *              rotation is fp32 with cosine and sine good to fp32 at any position
  * x, y       : DEVICE; y may be x (then with the same strides), and must not overlap it otherwise

@@ -1051,7 +1051,8 @@ lkv_status lkv_rope(lkv_ctx* ctx, const lkv_rotary* rotary, int32_t dtype, int32
   if (dtype != LKV_BF16 && dtype != LKV_FP32) return fail(ctx, LKV_ERR_INVALID_ARG, "unknown dtype %d", dtype);
   if (n_batch < 1 || n_heads < 1 || n_tokens < 1) return fail(ctx, LKV_ERR_INVALID_ARG, "n_batch, n_heads and n_tokens must be >= 1");
   if (head_dim != lkv::kHeadDim) return fail(ctx, LKV_ERR_UNSUPPORTED, "head_dim must be 128, got %d", head_dim);
-  if ((int64_t)n_batch * n_tokens >= (int64_t)1 << 31 || ((int64_t)n_batch * n_tokens / 32 + n_batch) * (n_heads / 4 + 1) >= (int64_t)1 << 31)
+  // a grid holds fewer than 2^32 threads
+  if ((int64_t)n_batch * n_tokens >= (int64_t)1 << 31 || lkv::rope_blocks(n_batch, n_heads, n_tokens) >= (int64_t)1 << 24)
     return fail(ctx, LKV_ERR_UNSUPPORTED, "n_batch * n_heads * n_tokens is too large for one launch");
   if (x == nullptr || y == nullptr || x_strides == nullptr || y_strides == nullptr)
     return fail(ctx, LKV_ERR_INVALID_ARG, "x, y, x_strides or y_strides is NULL");

@@ -122,6 +122,7 @@ hipError_t launch_quant_decode(int format, int G, const void* q, const QuantRows
 struct RopeStrides {   // in elements
   int64_t batch, head, token;
 };
+int64_t rope_blocks(int64_t n_batch, int64_t n_heads, int64_t n_tokens);
 void launch_rope(const RotaryArgs& rot, bool f32, const void* x, const RopeStrides& xs, void* y, const RopeStrides& ys,
                  const int32_t* positions, int64_t positions_stride, int first_position, int n_batch, int n_heads, int n_tokens,
                  bool backward, hipStream_t stream);

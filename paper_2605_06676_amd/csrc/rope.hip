@@ -197,17 +197,26 @@ rope_kernel(RotaryArgs rot, const T* x, RopeStrides xs, T* y, RopeStrides ys, co
   }
 }
 
+// Rows that a block may join, and blocks of a launch.
+static int64_t rope_run(int64_t n_batch, int64_t n_tokens) {
+  return n_tokens >= kRopeTokens ? n_tokens : n_batch * n_tokens;   // short ones are joined across batches
+}
+
+int64_t rope_blocks(int64_t n_batch, int64_t n_heads, int64_t n_tokens) {
+  const int64_t run = rope_run(n_batch, n_tokens);
+  return n_batch * n_tokens / run * ((run + kRopeTokens - 1) / kRopeTokens) * ((n_heads + kRopeHeads - 1) / kRopeHeads);
+}
+
 void launch_rope(const RotaryArgs& rot, bool f32, const void* x, const RopeStrides& xs, void* y, const RopeStrides& ys,
                  const int32_t* positions, int64_t positions_stride, int first_position, int n_batch, int n_heads, int n_tokens,
                  bool backward, hipStream_t stream) {
-  const uint32_t n_rows = (uint32_t)((int64_t)n_batch * n_tokens);
-  const uint32_t run = n_tokens >= kRopeTokens ? (uint32_t)n_tokens : n_rows;   // short ones are joined across batches
-  const uint32_t blocks = n_rows / run * ((run + kRopeTokens - 1) / kRopeTokens);
+  const uint32_t run = (uint32_t)rope_run(n_batch, n_tokens);
+  const uint32_t blocks = (uint32_t)rope_blocks(n_batch, n_heads, n_tokens);
   const uint32_t head_blocks = (uint32_t)(n_heads + kRopeHeads - 1) / kRopeHeads;
   const bool heads_inside = xs.head < xs.token;
   auto launch = [&](auto tag, auto layout) {
     using T = decltype(tag);
-    hipLaunchKernelGGL((rope_kernel<T, decltype(layout)::value>), dim3(blocks * head_blocks), dim3(kRopeThreads), 0, stream, rot,
+    hipLaunchKernelGGL((rope_kernel<T, decltype(layout)::value>), dim3(blocks), dim3(kRopeThreads), 0, stream, rot,
                        static_cast<const T*>(x), xs, static_cast<T*>(y), ys, positions, positions_stride, first_position,
                        (uint32_t)n_tokens, run, n_heads, head_blocks, heads_inside, backward ? -1.f : 1.f);
   };

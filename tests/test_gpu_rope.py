@@ -222,6 +222,7 @@ def test_refusals(ctx):
         call(1, xs=odd(i, 132)); call(1, ys=odd(i, 4))
         call(1, ys=odd(i, 0))
     call(1, b=ptr(x), ys=odd(2, 256)); call(1, backward=2); call(1, first=2 ** 31 - 2); call(2, n=(1 << 16, 1, 1 << 15))
+    call(2, n=(1 << 23, 1, 33)); call(2, n=(1, 1, 1 << 30))          # more blocks than a grid has
     call(1, rotary=bad(layout=3)); call(1, rotary=bad(rotary_dim=0)); call(1, rotary=bad(rotary_dim=7)); call(1, rotary=bad(rotary_dim=256))
     call(1, rotary=bad(inv_freq=None)); call(1, rotary=bad(factor=float("inf")))
     with pytest.raises(AssertionError):
