@@ -46,6 +46,7 @@ constexpr int kQdBlocks = 512;
 constexpr int kQdSomePieces = 4;        // blocks a segment from which the merge has 8, and
 constexpr int kQdManyPieces = 32;       // 32 half waves to a query head
 constexpr float kQdWeightUnit = 32768.f;   // weights of at most 1 times this: f16 holds steps of 2^-24, so 2^-39 of the largest weight
+constexpr float kQdLeastUnit = 0x1p-126f;  // of the sums: 1 / it is finite, whatever a block's scale
 constexpr float kQdLog2e = 1.4426950408889634f;
 constexpr float kQdLn2 = 0.6931471805599453f;
 
@@ -201,7 +202,7 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
   for (;;) {
   const QdPiece now = next;
   float m_run = -INFINITY, l_run = 0.f;   // running maximum of head c (log2 domain) in its four lanes, this lane's share of the denominator
-  float vs_run = 0.f;                     // largest value scale so far: the sums are in units of it
+  float vs_run = kQdLeastUnit;            // largest value scale so far: the sums are in units of it
   f32x4_t acc[8];                         // O[head 4 r + e][channel 8 c + m], in units of vs_run / kQdWeightUnit
 #pragma unroll
   for (int m = 0; m < 8; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -266,9 +267,9 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
     for (int i = 0; i < 8; ++i) { p[i] = qd_exp2(p[i] - mx); psum += p[i]; }
     l_run = l_run * alpha + psum;
     const float vs_new = fmaxf(vs_run, vs);
-    const float unit = vs_new > 0.f ? 1.f / vs_new : 0.f;
+    const float unit = 1.f / vs_new;
     const float ratio = vs * unit * kQdWeightUnit;
-    alpha *= vs_run * unit;
+    if (vs > vs_run) alpha *= vs_run * unit;   // x (1 / x) can be 1 - 2^-24, which would add up over the tiles
     vs_run = vs_new;
     f16x8_t phigh, plow;   // the weights of the values' codes, at most kQdWeightUnit: rounded to f16, and what the rounding left
 #pragma unroll

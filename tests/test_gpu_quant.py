@@ -272,6 +272,44 @@ def test_decode_with_scales_of_any_kind(ctx, fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+def test_decode_with_scales_below_the_normal_numbers(ctx, fmt):
+    lengths = [40, 100, 33, 64]
+    p, cap = _filled(lengths, 5, fmt, 17)
+    own = np.flatnonzero(p.ks != GUARD_SCALE)
+    tiny = [1e-40, 3e-39, 2.0 ** -149, 1e-40, 0.0, 0.25, 1e-40, 2e-42, 1e-40, 2.0 ** -149]   # 2 + 4 + 2 + 2 blocks
+    assert len(own) == len(tiny)
+    p.vs[own] = np.float32(tiny)
+    p.ks[own[::2]] = np.float32(1e-42)
+    p.upload()
+    q = _queries(1, 1, 8, 18)
+    out, lse = _decode(ctx, p, cap, lengths, q, 4, 128 ** -0.5)
+    _assert_decode(p, cap, lengths, q, 4, 128 ** -0.5, out, lse)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_decode_with_one_scale_of_no_power_of_two_in_many_blocks(ctx, fmt):
+    """A wave with 1024 tiles, the same scale c in all of them, where c (1 / c) is 1 - 2^-24: nothing may be lost from tile to tile.
+    All scores are 0 and the codes are small whole numbers, so that their sums times 2^15 are exact.  What is off: the weights,
+    1 / c and its product with c and the second parts that the sums swallow, 3 * 2^-24; c and the quotient at the end, 2 * 2^-24."""
+    c, n = np.float32(0.013), 32 * 1024
+    assert c * (np.float32(1.0) / c) != 1
+    rows = 2048 * 1024 * 32 - 32          # spare but for the first n; 2048 waves have 1024 blocks each
+    codes = np.array([0x38, 0x40, 0x44, 0x48], dtype=np.uint8) if fmt == Q.E4M3 else np.array([1, 2, 3, 4], dtype=np.uint8)
+    pick = np.random.default_rng(19).integers(0, 4, (n, 128))
+    k, v = (torch.empty((rows, 128), dtype=torch.uint8, device="cuda") for _ in range(2))
+    k[:n].zero_()
+    v[:n].copy_(torch.from_numpy(codes[pick]))
+    ks, vs = (torch.full((Q.scale_count(1, rows),), float(c), device="cuda") for _ in range(2))
+    p = lkv.QuantRows(k.view(KINDS[fmt]), v.view(KINDS[fmt]), ks, vs)
+    q = _queries(1, 1, 2, 20).cuda()
+    ws = torch.empty((lkv.lkv_decode_quant_workspace_bytes(1, rows, 2, 1),), dtype=torch.uint8, device="cuda")
+    out = torch.full((1, 1, 2, 128), float("nan"), device="cuda")
+    lkv.lkv_decode_attn_quant(ctx, 1, 1, 1, 2, 128, q, p, i32([0, rows]), i32([n]), rows, 128 ** -0.5, out, None, ws)
+    ref = (pick + 1).mean(axis=0) * float(c)
+    assert np.abs(out.cpu().numpy()[0, 0] / ref - 1).max() <= 5 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("ahead", [0.0, 3.0, 10.5, 14.0, 18.0])
 def test_decode_of_one_large_weight_and_many_small_ones(ctx, fmt, ahead):
     """One row is `ahead` in its score and has value 0, fifty thousand have score 0 and value 1: what the output holds comes from
