@@ -5,7 +5,7 @@
 // rows finds the segment.  Sixteen lanes hold a row, 16 bytes each, so that the block's 32 + 32 rows of K and V are sixteen
 // 16-byte loads of every lane, all in flight together, and stay in registers: the largest magnitude is a maximum over them (on
 // the bit patterns, two at a time) and over the lanes, and each piece of 8 values leaves as 8 codes.  The data is
-// read once and written once (512 + 256 bytes a row), which bounds the kernel: 1.24 million rows of 32 x 8 heads 158 us, 6.0 TB/s
+// read once and written once (512 + 256 bytes a row), which bounds the kernel: 1.24 million rows of 32 x 8 heads 156 us, 6.1 TB/s
 // in and out (176 us with stores that stay in the caches, 168 us with eight waves a block); a re-eviction's gather of 1.0
 // million rows from 8 bits to 8 bits 90 us, 5.8 TB/s.
 #include <cstring>

@@ -4,10 +4,10 @@
 // Work decomposition.  The scale numbers count the tiles of 32 rows through all segments, so they are a flat list of equal work: wave
 // w takes numbers [w n, (w + 1) n), whatever segments they belong to, and n is chosen so that the launch is one round of resident
 // waves.  A search over the segments' first numbers finds where a wave starts; from there it walks from segment to segment, and
-// the rows of a segment in its range are a piece.  A piece that is a whole segment is finished by its wave; other pieces go to workspace slot
-// (wave + segment), which is a slot of their own because both grow along the rows, except that the four waves of a block that
-// lies inside one segment merge their pieces in LDS into one.  A second kernel merges the slots of each segment.  A segment always has a number, where an
-// empty one gets its zeros.
+// the rows of a segment in its range are a piece.  A piece that is a whole segment is finished by its wave; other pieces go to
+// workspace slot (wave + segment), which is a slot of their own because both grow along the rows, except that the four waves of
+// a block that lies inside one segment merge their pieces in LDS into one.  A second kernel merges the slots of each segment.  A
+// segment always has a number, where an empty one gets its zeros.
 // (Chunks of a segment's rows dealt to blocks, a power of two of rows each, left a third of the waves idle: 256 segments of 1.26
 // million rows 71.7 us with the best chunk, 105.5 with twice as many rows in it.)
 //
@@ -18,14 +18,15 @@
 // The first product's operand needs 8 channels of a token in a lane: a sum over channels may take them in any order, so a lane takes
 // 16 contiguous bytes of its token's row for two steps and Q's operand is read in that order.  Loaded so from memory, neighbouring
 // lanes would read different rows; whole rows are loaded, 8 to an instruction, and change lanes through LDS (256 segments of 1.26
-// million rows 63.9 -> 61.9 us, 896 of 2.9 million 139.9 -> 134.7).  The second needs 8 tokens of a channel in a lane: it loads 8 bytes, 8 channels, of each of the 8 tokens whose scores the
-// first product left with it, and byte permutes (16 for a tile) put the same channel of two tokens side by side, which convert
-// together; column c of the m-th product then is channel 8 c + m, and a lane ends with 8 contiguous channels of the output.
+// million rows 63.9 -> 61.9 us, 896 of 2.9 million 139.9 -> 134.7).  The second needs 8 tokens of a channel in a lane: it loads 8
+// bytes, 8 channels, of each of the 8 tokens whose scores the first product left with it, and byte permutes (16 for a tile) put
+// the same channel of two tokens side by side, which convert together; column c of the m-th product then is channel 8 c + m, and a
+// lane ends with 8 contiguous channels of the output.
 // Softmax runs in fp32 in the log2 domain.  The weights of the values' codes are at most 1, since the sums are kept in units of the
 // largest value scale so far; times 2^15 they are rounded to f16 and what that left is multiplied too, which holds 22 bits of them,
-// fewer only below 2^-18 of the largest one, where the step of 2^-39 weighs in
-// (error of the output against 64 bits 2e-7; with two bf16 parts, 16 bits, it was 1.1e-6; without the 2^15, an output that fifty thousand weights of
-// e^-18 make up was off by 6e-4).
+// fewer only below 2^-18 of the largest one, where the step of 2^-39 weighs in (error of the output against 64 bits 2e-7; with
+// two bf16 parts, 16 bits, it was 1.1e-6; without the 2^15, an output that fifty thousand weights of e^-18 make up was off by
+// 6e-4).
 //
 // Bound by the stream of the rows: 1.26 million rows of 256 segments 54.4 us (5.9 TB/s) and 5 us for the merge; 2.9 million of
 // 896 in int8 128 us (5.9 TB/s).
@@ -200,181 +201,181 @@ quant_decode_kernel(const uint16_t* __restrict__ q, QuantRows rows, const int32_
   load_values(row0, last, number);
 #pragma unroll 1
   for (;;) {
-  const QdPiece now = next;
-  float m_run = -INFINITY, l_run = 0.f;   // running maximum of head c (log2 domain) in its four lanes, this lane's share of the denominator
-  float vs_run = kQdLeastUnit;            // largest value scale so far: the sums are in units of it
-  f32x4_t acc[8];                         // O[head 4 r + e][channel 8 c + m], in units of vs_run / kQdWeightUnit
+    const QdPiece now = next;
+    float m_run = -INFINITY, l_run = 0.f;   // running maximum of head c (log2 domain) in its four lanes, this lane's share of the denominator
+    float vs_run = kQdLeastUnit;            // largest value scale so far: the sums are in units of it
+    f32x4_t acc[8];                         // O[head 4 r + e][channel 8 c + m], in units of vs_run / kQdWeightUnit
 #pragma unroll
-  for (int m = 0; m < 8; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  next = next_piece(now.s + 1);   // while the rows are on their way
-  // waited for here: inside the loop the wait would reach the rows to come as well
+    for (int m = 0; m < 8; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    next = next_piece(now.s + 1);   // while the rows are on their way
+    // waited for here: inside the loop the wait would reach the rows to come as well
 #pragma unroll
-  for (int w = 0; w < 2; ++w) asm volatile("" : "+v"(qfrag[w][0]), "+v"(qfrag[w][1]));
+    for (int w = 0; w < 2; ++w) asm volatile("" : "+v"(qfrag[w][0]), "+v"(qfrag[w][1]));
 
-  // One set of registers a tile: the next tile's keys are asked for when this one's have been multiplied, its values likewise.
+    // One set of registers a tile: the next tile's keys are asked for when this one's have been multiplied, its values likewise.
 #pragma unroll 1
-  for (int t = now.tile; t < now.end; ++t) {
-    // The keys change lanes through LDS: token t's piece p lies at p ^ (t / 2 & 7) of its row, where both sides meet all banks.
-    const float ts = qscale * ks;
-    uint8_t* tile = key_lds[wave];
+    for (int t = now.tile; t < now.end; ++t) {
+      // The keys change lanes through LDS: token t's piece p lies at p ^ (t / 2 & 7) of its row, where both sides meet all banks.
+      const float ts = qscale * ks;
+      uint8_t* tile = key_lds[wave];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<uint4*>(tile + (8 * i + (lane >> 3)) * kHeadDim + 16 * ((lane & 7) ^ ((4 * i + (lane >> 4)) & 7))) = kk[i];
-    // Asked for in any case, so that the waits for this tile's values can count the loads behind them; behind a wave's last
-    // tile it is one row of it again.
-    if (t + 1 < now.end) {
-      row0 += kQdTile;
-      last -= kQdTile;
-      ++number;
-    } else if (next.s >= 0) {
-      row0 = (int64_t)next.cap + next.tile * kQdTile;
-      last = next.len - next.tile * kQdTile - 1;
-      number = quant_first_scale(next.cap, next.s) + next.tile;
-    } else {
-      last = 0;
-    }
-    load_keys(row0, last, number);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    f32x4_t sacc[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      sacc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const uint4 k = *reinterpret_cast<const uint4*>(tile + (16 * h + c) * kHeadDim + 16 * ((4 * w + r) ^ (c >> 1)));
-        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(k.x, k.y), qfrag[w][0], sacc[h], 0, 0, 0);
-        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(k.z, k.w), qfrag[w][1], sacc[h], 0, 0, 0);
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint4*>(tile + (8 * i + (lane >> 3)) * kHeadDim + 16 * ((lane & 7) ^ ((4 * i + (lane >> 4)) & 7))) = kk[i];
+      // Asked for in any case, so that the waits for this tile's values can count the loads behind them; behind a wave's last
+      // tile it is one row of it again.
+      if (t + 1 < now.end) {
+        row0 += kQdTile;
+        last -= kQdTile;
+        ++number;
+      } else if (next.s >= 0) {
+        row0 = (int64_t)next.cap + next.tile * kQdTile;
+        last = next.len - next.tile * kQdTile - 1;
+        number = quant_first_scale(next.cap, next.s) + next.tile;
+      } else {
+        last = 0;
       }
-    }
-    float p[8];
-    float mx = m_run;
+      load_keys(row0, last, number);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      f32x4_t sacc[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = sacc[i >> 2][i & 3] * ts;
-    if ((t + 1) * kQdTile > now.len) {   // the segment's last tile
+      for (int h = 0; h < 2; ++h) {
+        sacc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (t * kQdTile + 16 * (i >> 2) + 4 * r + (i & 3) >= now.len) p[i] = -INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, p[i]);
-    mx = max_over_row_blocks(mx);
-    float alpha = qd_exp2(m_run - mx);   // 0 on the first tile
-    m_run = mx;
-    float psum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { p[i] = qd_exp2(p[i] - mx); psum += p[i]; }
-    l_run = l_run * alpha + psum;
-    const float vs_new = fmaxf(vs_run, vs);
-    const float unit = 1.f / vs_new;
-    const float ratio = vs * unit * kQdWeightUnit;
-    if (vs > vs_run) alpha *= vs_run * unit;   // x (1 / x) can be 1 - 2^-24, which would add up over the tiles
-    vs_run = vs_new;
-    f16x8_t phigh, plow;   // the weights of the values' codes, at most kQdWeightUnit: rounded to f16, and what the rounding left
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float w = p[i] * ratio;
-      phigh[i] = (_Float16)w;
-      plow[i] = (_Float16)(w - (float)phigh[i]);
-    }
-    if (__ballot(alpha != 1.f) != 0ull) {   // a maximum moved: the sums' rows are heads 4 r + e
-      float al[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) al[e] = __shfl(alpha, 4 * r + e, 64);
-#pragma unroll
-      for (int m = 0; m < 8; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[m][e] *= al[e];
-    }
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {   // channels 8 c + 4 b .. + 3
-      // bytes of two tokens' four channels, side by side: [token pair][channels 4 b, 4 b + 1 or 4 b + 2, 4 b + 3]
-      uint32_t two[4][2];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint2 first = vv[i >> 1][2 * (i & 1)], second = vv[i >> 1][2 * (i & 1) + 1];
-        uint32_t x = b == 0 ? first.x : first.y, y = b == 0 ? second.x : second.y;
-        two[i][0] = __builtin_amdgcn_perm(y, x, 0x05010400u);
-        two[i][1] = __builtin_amdgcn_perm(y, x, 0x07030602u);
-        if constexpr (kFormat == kQuantInt8) {
-          two[i][0] ^= 0x80808080u;
-          two[i][1] ^= 0x80808080u;
+        for (int w = 0; w < 2; ++w) {
+          const uint4 k = *reinterpret_cast<const uint4*>(tile + (16 * h + c) * kHeadDim + 16 * ((4 * w + r) ^ (c >> 1)));
+          sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(k.x, k.y), qfrag[w][0], sacc[h], 0, 0, 0);
+          sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_operand<kFormat>(k.z, k.w), qfrag[w][1], sacc[h], 0, 0, 0);
         }
       }
+      float p[8];
+      float mx = m_run;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint4 w;
-        if (i % 2 == 0)
-          w = make_uint4(two_values<kFormat, false>(two[0][i / 2]), two_values<kFormat, false>(two[1][i / 2]),
-                         two_values<kFormat, false>(two[2][i / 2]), two_values<kFormat, false>(two[3][i / 2]));
-        else
-          w = make_uint4(two_values<kFormat, true>(two[0][i / 2]), two_values<kFormat, true>(two[1][i / 2]),
-                         two_values<kFormat, true>(two[2][i / 2]), two_values<kFormat, true>(two[3][i / 2]));
-        const f16x8_t vb = __builtin_bit_cast(f16x8_t, w);
-        acc[4 * b + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(phigh, vb, acc[4 * b + i], 0, 0, 0);
-        acc[4 * b + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(plow, vb, acc[4 * b + i], 0, 0, 0);
+      for (int i = 0; i < 8; ++i) p[i] = sacc[i >> 2][i & 3] * ts;
+      if ((t + 1) * kQdTile > now.len) {   // the segment's last tile
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (t * kQdTile + 16 * (i >> 2) + 4 * r + (i & 3) >= now.len) p[i] = -INFINITY;
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, p[i]);
+      mx = max_over_row_blocks(mx);
+      float alpha = qd_exp2(m_run - mx);   // 0 on the first tile
+      m_run = mx;
+      float psum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { p[i] = qd_exp2(p[i] - mx); psum += p[i]; }
+      l_run = l_run * alpha + psum;
+      const float vs_new = fmaxf(vs_run, vs);
+      const float unit = 1.f / vs_new;
+      const float ratio = vs * unit * kQdWeightUnit;
+      if (vs > vs_run) alpha *= vs_run * unit;   // x (1 / x) can be 1 - 2^-24, which would add up over the tiles
+      vs_run = vs_new;
+      f16x8_t phigh, plow;   // the weights of the values' codes, at most kQdWeightUnit: rounded to f16, and what the rounding left
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float w = p[i] * ratio;
+        phigh[i] = (_Float16)w;
+        plow[i] = (_Float16)(w - (float)phigh[i]);
+      }
+      if (__ballot(alpha != 1.f) != 0ull) {   // a maximum moved: the sums' rows are heads 4 r + e
+        float al[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) al[e] = __shfl(alpha, 4 * r + e, 64);
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[m][e] *= al[e];
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {   // channels 8 c + 4 b .. + 3
+        // bytes of two tokens' four channels, side by side: [token pair][channels 4 b, 4 b + 1 or 4 b + 2, 4 b + 3]
+        uint32_t two[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint2 first = vv[i >> 1][2 * (i & 1)], second = vv[i >> 1][2 * (i & 1) + 1];
+          uint32_t x = b == 0 ? first.x : first.y, y = b == 0 ? second.x : second.y;
+          two[i][0] = __builtin_amdgcn_perm(y, x, 0x05010400u);
+          two[i][1] = __builtin_amdgcn_perm(y, x, 0x07030602u);
+          if constexpr (kFormat == kQuantInt8) {
+            two[i][0] ^= 0x80808080u;
+            two[i][1] ^= 0x80808080u;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint4 w;
+          if (i % 2 == 0)
+            w = make_uint4(two_values<kFormat, false>(two[0][i / 2]), two_values<kFormat, false>(two[1][i / 2]),
+                           two_values<kFormat, false>(two[2][i / 2]), two_values<kFormat, false>(two[3][i / 2]));
+          else
+            w = make_uint4(two_values<kFormat, true>(two[0][i / 2]), two_values<kFormat, true>(two[1][i / 2]),
+                           two_values<kFormat, true>(two[2][i / 2]), two_values<kFormat, true>(two[3][i / 2]));
+          const f16x8_t vb = __builtin_bit_cast(f16x8_t, w);
+          acc[4 * b + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(phigh, vb, acc[4 * b + i], 0, 0, 0);
+          acc[4 * b + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(plow, vb, acc[4 * b + i], 0, 0, 0);
+        }
+      }
+      load_values(row0, last, number);
     }
-    load_values(row0, last, number);
-  }
 #pragma unroll
-  for (int m = 0; m < 8; ++m)
+    for (int m = 0; m < 8; ++m)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[m][e] *= vs_run * (1.f / kQdWeightUnit);
-  if (next.s >= 0) load_q(next);
-  l_run = sum_over_row_blocks(l_run);
-  if (together) {   // the only piece of each wave
-    const int per = G * kHeadDim;
-    float* m_lds = merge_lds + kQdWaves * per;
-    float* l_lds = m_lds + kQdWaves * G;
-    if (r == 0 && c < G) { m_lds[wave * G + c] = m_run; l_lds[wave * G + c] = l_run; }
+      for (int e = 0; e < 4; ++e) acc[m][e] *= vs_run * (1.f / kQdWeightUnit);
+    if (next.s >= 0) load_q(next);
+    l_run = sum_over_row_blocks(l_run);
+    if (together) {   // the only piece of each wave
+      const int per = G * kHeadDim;
+      float* m_lds = merge_lds + kQdWaves * per;
+      float* l_lds = m_lds + kQdWaves * G;
+      if (r == 0 && c < G) { m_lds[wave * G + c] = m_run; l_lds[wave * G + c] = l_run; }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int h = 4 * r + e;
+        if (h < G) {
+          float4* dst = reinterpret_cast<float4*>(merge_lds + wave * per + h * kHeadDim + 8 * c);
+          dst[0] = make_float4(acc[0][e], acc[1][e], acc[2][e], acc[3][e]);
+          dst[1] = make_float4(acc[4][e], acc[5][e], acc[6][e], acc[7][e]);
+        }
+      }
+      __syncthreads();
+      const size_t slot = (size_t)blockIdx.x * kQdWaves + now.s;
+      for (int o = tid; o < per; o += kQdThreads) {
+        const int h = o / kHeadDim;
+        float mx = m_lds[h];
+#pragma unroll
+        for (int w = 1; w < kQdWaves; ++w) mx = fmaxf(mx, m_lds[w * G + h]);
+        float num = 0.f, den = 0.f;
+#pragma unroll
+        for (int w = 0; w < kQdWaves; ++w) {
+          const float weight = qd_exp2(m_lds[w * G + h] - mx);
+          num = fmaf(merge_lds[w * per + o], weight, num);
+          den = fmaf(l_lds[w * G + h], weight, den);
+        }
+        ws_acc[slot * per + o] = num;
+        if (o % kHeadDim == 0) { ws_m[slot * G + h] = mx; ws_l[slot * G + h] = den; }
+      }
+      return;
+    }
+    const bool whole = now.tile == 0 && now.end * kQdTile >= now.len;
+    const size_t slot = (size_t)wave_id + now.s;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int h = 4 * r + e;
+      const float mxh = __shfl(m_run, h, 64), den = __shfl(l_run, h, 64);   // head h's are in lane h
       if (h < G) {
-        float4* dst = reinterpret_cast<float4*>(merge_lds + wave * per + h * kHeadDim + 8 * c);
-        dst[0] = make_float4(acc[0][e], acc[1][e], acc[2][e], acc[3][e]);
-        dst[1] = make_float4(acc[4][e], acc[5][e], acc[6][e], acc[7][e]);
+        const float by = whole ? 1.f / den : 1.f;
+        float4* dst = reinterpret_cast<float4*>((whole ? out + ((size_t)now.s * G + h) * kHeadDim : ws_acc + (slot * G + h) * kHeadDim) + 8 * c);
+        dst[0] = make_float4(acc[0][e] * by, acc[1][e] * by, acc[2][e] * by, acc[3][e] * by);
+        dst[1] = make_float4(acc[4][e] * by, acc[5][e] * by, acc[6][e] * by, acc[7][e] * by);
+        if (c == 0) {
+          if (!whole) { ws_m[slot * G + h] = mxh; ws_l[slot * G + h] = den; }
+          else if (lse != nullptr) lse[(size_t)now.s * G + h] = mxh * kQdLn2 + __logf(den);
+        }
       }
     }
-    __syncthreads();
-    const size_t slot = (size_t)blockIdx.x * kQdWaves + now.s;
-    for (int o = tid; o < per; o += kQdThreads) {
-      const int h = o / kHeadDim;
-      float mx = m_lds[h];
-#pragma unroll
-      for (int w = 1; w < kQdWaves; ++w) mx = fmaxf(mx, m_lds[w * G + h]);
-      float num = 0.f, den = 0.f;
-#pragma unroll
-      for (int w = 0; w < kQdWaves; ++w) {
-        const float weight = qd_exp2(m_lds[w * G + h] - mx);
-        num = fmaf(merge_lds[w * per + o], weight, num);
-        den = fmaf(l_lds[w * G + h], weight, den);
-      }
-      ws_acc[slot * per + o] = num;
-      if (o % kHeadDim == 0) { ws_m[slot * G + h] = mx; ws_l[slot * G + h] = den; }
-    }
-    return;
-  }
-  const bool whole = now.tile == 0 && now.end * kQdTile >= now.len;
-  const size_t slot = (size_t)wave_id + now.s;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int h = 4 * r + e;
-    const float mxh = __shfl(m_run, h, 64), den = __shfl(l_run, h, 64);   // head h's are in lane h
-    if (h < G) {
-      const float by = whole ? 1.f / den : 1.f;
-      float4* dst = reinterpret_cast<float4*>((whole ? out + ((size_t)now.s * G + h) * kHeadDim : ws_acc + (slot * G + h) * kHeadDim) + 8 * c);
-      dst[0] = make_float4(acc[0][e] * by, acc[1][e] * by, acc[2][e] * by, acc[3][e] * by);
-      dst[1] = make_float4(acc[4][e] * by, acc[5][e] * by, acc[6][e] * by, acc[7][e] * by);
-      if (c == 0) {
-        if (!whole) { ws_m[slot * G + h] = mxh; ws_l[slot * G + h] = den; }
-        else if (lse != nullptr) lse[(size_t)now.s * G + h] = mxh * kQdLn2 + __logf(den);
-      }
-    }
-  }
-  if (next.s < 0) return;
+    if (next.s < 0) return;
   }
 }
 
@@ -503,7 +504,8 @@ hipError_t launch_quant_decode(int format, int G, const void* q, const QuantRows
     constexpr int kParts = decltype(tag)::value;
     const int n_heads = n_segments * G;
     hipLaunchKernelGGL((quant_decode_merge_kernel<kParts>), dim3(kParts == 1 ? (n_heads + kQdHalves - 1) / kQdHalves : n_heads),
-                       dim3(kParts == 1 ? kQdThreads : kParts * kQdHalf), 0, stream, cap, lengths, n_heads, shape.per_wave, G, ws_acc, ws_m, ws_l, out, lse);
+                       dim3(kParts == 1 ? kQdThreads : kParts * kQdHalf), 0, stream, cap, lengths, n_heads, shape.per_wave, G, ws_acc,
+                       ws_m, ws_l, out, lse);
   };
   if (shape.blocks > kQdManyPieces * n_segments) merge(std::integral_constant<int, 32>{});
   else if (shape.blocks > kQdSomePieces * n_segments) merge(std::integral_constant<int, kQdHalves>{});
